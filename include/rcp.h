@@ -557,6 +557,86 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
                                 float softmax_scale, void* out, rcp_dtype out_dtype,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Paged 8-bit KV cache: new tokens of many sequences at once, prompts and single tokens alike, with lengths and page tables in DEVICE
+ * memory, so that a captured HIP graph follows them.
+ *
+ * Layout of one cached tensor (keys or values) of one layer: a pool of n_pages pages of `page` tokens (16, 32, 64 or 128) of H heads of
+ * D elements (64 or 128)
+ *   codes   [n_pages][H][page][D]  E4M3 bytes (OCP: 4 exponent and 3 mantissa bits, largest value 448, no infinities)
+ *   scales  [n_pages][H]           binary32; a code c stands for c times the scale of its page and head
+ *
+ * rcp_kv8_batch: which sequences a call is about, all arrays on the device.
+ *   rows       new tokens of the call (k, v, q and out have that many rows)
+ *   starts     [sequences + 1], or NULL: one new token for each sequence, rows == sequences.  Rows starts[b] .. starts[b + 1] - 1 are the new
+ *              tokens of sequence b, in order; ascending within 0 .. rows (other values are cut to that, row by row).  Rows
+ *              before starts[0] and from starts[sequences] on belong to no sequence: nothing is written for them.
+ *   lengths    [sequences]: tokens of the sequence INCLUDING the new ones; new token i of n has position lengths[b] - n + i
+ *   table      [sequences][width]: page of positions page * j .. of sequence b at table[b][j].  An entry outside 0 .. n_pages - 1
+ *              is no page: its tokens are neither stored nor attended to.  Positions from width * page on have no page.
+ * Sequences may share pages that no call writes; a page that a call writes belongs to one of its sequences (otherwise which of
+ * their tokens it holds is unspecified).
+ *
+ * rcp_kv8_append: k, v are `rows` tokens of H heads of D elements of `x_dtype`, a head's elements and a token's heads adjacent, tokens
+ *   k_stride / v_stride elements apart (multiples of 8, at least H * D when rows > 1: views of one projection's output fit).
+ *   rope_or_null: device [width * page][D] binary32, the cosines and then the sines of the D/2 angles of a position; the keys (and
+ *   queries) are rotated first: y_j = x_j c_j - x_{j+D/2} s_j, y_{j+D/2} = x_{j+D/2} c_j + x_j s_j, products and sums rounded on their
+ *   own.  rotate != 0: then the normalised order-D Hadamard transform of every key (and query) head, as rcp_kv4_append has it.
+ *   Per page and head: scale = 2^E, E the smallest exponent with which no finite magnitude of the new tokens exceeds 448 * 2^E, within
+ *   -40 .. 120; codes = x / scale to the nearest, ties to even, an infinity as 448 of its sign, a NaN as 0.  A page whose slot 0 is among the new tokens starts
+ *   anew (what it held is ignored); another one keeps the larger of its scale and the new one, and where that grows the codes before the first new token are
+ *   rounded to the new scale.  Slots behind the last new token keep their bytes.
+ *   q_or_null: `rows` tokens of H_q heads, q_stride apart, rotated likewise into q_out ([rows][H_q][D] of x_dtype, rounded once; may be q
+ *   itself when q is dense).  Rows without a position in the table are left as they are in q_out.
+ *
+ * rcp_kv8_attn: row i of sequence b attends to the cached tokens of b at positions 0 .. its own:
+ *     out[i][h] = sum_t softmax_t(softmax_scale * q[i][h] . K[g][t]) * V[g][t],   g = h / (H_q / H)
+ *   q: [rows][H_q][D] of `q_dtype`; out: [rows][H_q][D] of `out_dtype` (any rcp_dtype).  A row that sees no token (an empty sequence, no
+ *   page) gets zeros.  Tokens behind a row's own never enter, whatever bytes their slots hold; codes within a sequence must not be NaN
+ *   (rcp_kv8_append writes none).  Sums are binary32.  The softmax weights enter the product with the values as binary16 numbers, or
+ *   as pairs of them (22 bits) for binary32 results and, with one token a sequence, binary16 ones; a binary32 query as pairs, scaled by its largest element.
+ *   workspace: rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, starts == NULL) bytes, overwritten by every call.  Calls that
+ *   may overlap need workspaces of their own.
+ * Limits: sequences <= 1024, sequences * width * page < 2^31, H_q <= 4096, rows <= 2^20 (RCP_ERR_SHAPE).
+ */
+typedef struct {
+    void* k_codes;
+    float* k_scales;
+    void* v_codes;
+    float* v_scales;
+    int n_pages, H, page, D;
+} rcp_kv8_cache;
+typedef struct {
+    const int32_t* starts_or_null;
+    const int32_t* lengths;
+    const int32_t* table;
+    int rows, sequences, width;
+} rcp_kv8_batch;
+#define RCP_KV8_MAX_SEQUENCES 1024
+#define RCP_KV8_MAX_ROWS (1 << 20)
+int rcp_kv8_append(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, rcp_dtype x_dtype, const float* rope_or_null, int rotate,
+                   const void* q_or_null, int64_t q_stride, int H_q, void* q_out_or_null, void* stream);
+size_t rcp_kv8_workspace_bytes(int rows, int sequences, int H_q, int H, int D, int one_token_each);
+int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const void* q, rcp_dtype q_dtype, int H_q,
+                 float softmax_scale, void* out, rcp_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection (rcp_w2a4_gemv and its kin give `base`):
+ *     out[m] = base[m] + scaling[a] * (x[m] A[a]^T) B[a]^T,   a = which[m]
+ * x: [M][K]; A: [adapters][r][K]; B: [adapters][N][r], all of `x_dtype` (RCP_F16 or RCP_BF16).  which: int32 [M] on the device; an entry
+ * outside 0 .. adapters - 1 is no adapter: out[m] = base[m].  scaling: binary32 [adapters].  base, out: [M][N] of `out_dtype` (any
+ * rcp_dtype); out may be base itself.  The inner product x A^T is held in binary32 (sums in a fixed order) and multiplied by B with
+ * at least 22 bits.  r a multiple of 8 up to RCP_LOWRANK_MAX_R, K a multiple of 32, N of 4 (RCP_ERR_SHAPE).
+ * workspace: rcp_lowrank_workspace_bytes(M, N, K, r) bytes, overwritten by every call.
+ */
+#define RCP_LOWRANK_MAX_R 128
+#define RCP_LOWRANK_MAX_M (1 << 19)
+size_t rcp_lowrank_workspace_bytes(int M, int N, int K, int r);
+int rcp_lowrank_add(const void* x, rcp_dtype x_dtype, int M, int N, int K, int r, int adapters, const void* A, const void* B,
+                    const int32_t* which, const float* scaling, const void* base, void* out, rcp_dtype out_dtype,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

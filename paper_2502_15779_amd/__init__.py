@@ -90,6 +90,16 @@ class GemvStep:
                            opt(xq_out, "xq_out"), opt(scale_out, "scale_out"))
 
 
+class _Kv8Cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int), ("H", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int)]
+
+
+class _Kv8Batch(ctypes.Structure):
+    _fields_ = [("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p), ("rows", ctypes.c_int),
+                ("sequences", ctypes.c_int), ("width", ctypes.c_int)]
+
+
 def _step_array(steps):
     arr = (_GemvStep * len(steps))()
     for i, s in enumerate(steps):
@@ -218,6 +228,18 @@ def lib():
         L.rcp_kv4_attn_decode.restype = ci
         L.rcp_kv4_attn_decode.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, ctypes.c_float, vp, ci, vp,
                                           ctypes.c_size_t, vp]
+        cl = ctypes.c_int64
+        cache, batch = ctypes.POINTER(_Kv8Cache), ctypes.POINTER(_Kv8Batch)
+        L.rcp_kv8_append.restype = ci
+        L.rcp_kv8_append.argtypes = [cache, batch, vp, cl, vp, cl, ci, vp, ci, vp, cl, ci, vp, vp]
+        L.rcp_kv8_workspace_bytes.restype = cz
+        L.rcp_kv8_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+        L.rcp_kv8_attn.restype = ci
+        L.rcp_kv8_attn.argtypes = [cache, batch, vp, ci, ci, ctypes.c_float, vp, ci, vp, cz, vp]
+        L.rcp_lowrank_workspace_bytes.restype = cz
+        L.rcp_lowrank_workspace_bytes.argtypes = [ci, ci, ci, ci]
+        L.rcp_lowrank_add.restype = ci
+        L.rcp_lowrank_add.argtypes = [vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, cz, vp]
         _lib = L
     return _lib
 
@@ -442,3 +464,42 @@ def kv4_attn_decode_batched(q, lengths, k_codes, k_params, v_codes, v_params, so
     [B*H_kv, S_max, ...] -> out [B, H_q, 128]."""
     return _host.kv4_attn_decode_batched(q, lengths, k_codes, k_params, v_codes, v_params, softmax_scale, out, out_dtype,
                                          workspace)
+
+
+# ---- paged 8-bit KV cache ----------------------------------------------------------------------
+def kv8_new_cache(n_pages, H, device, page=64, head_dim=128):
+    """(codes float8_e4m3fn [n_pages, H, page, head_dim], scales float32 [n_pages, H]) zero-filled device buffers: the pages of one
+    layer's keys, or values."""
+    return (torch.zeros((n_pages, H, page, head_dim), dtype=torch.float8_e4m3fn, device=device),
+            torch.zeros((n_pages, H), dtype=torch.float32, device=device))
+
+
+def kv8_append(k, v, lengths, table, k_codes, k_scales, v_codes, v_scales, starts=None, rope=None, rotate=False, q=None, q_out=None):
+    """New keys and values k, v [rows, H, D] of several sequences into the pages that table int32 [sequences, width] names; lengths
+    int32 [sequences] counts the new tokens in.  starts int32 [sequences + 1]: rows starts[b] .. starts[b + 1] - 1 belong to sequence b;
+    None: one row for each sequence.  rope float32 [positions, D] (cosines, then sines): the position rotation of keys and queries;
+    rotate: then the order-D Hadamard transform of both.  q [rows, H_q, D]: the queries, rotated into q_out, which is returned.
+    k, v and q may be views of one projection's output (tokens apart, heads of a token side by side)."""
+    return _host.kv8_append(k, v, lengths, table, k_codes, k_scales, v_codes, v_scales, starts, rope, rotate, q, q_out)
+
+
+def kv8_workspace_bytes(rows, sequences, H_q, H, D, one_token_each):
+    return int(lib().rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, 1 if one_token_each else 0))
+
+
+def kv8_attn(q, lengths, table, k_codes, k_scales, v_codes, v_scales, softmax_scale, starts=None, out=None, out_dtype=torch.float32,
+             workspace=None):
+    """q [rows, H_q, D]: every row attends to the cached tokens of its sequence up to its own position -> out [rows, H_q, D]; lengths, table
+    and starts as for kv8_append.  Rows of no sequence are left as they are in `out` (zeros where it is made here)."""
+    return _host.kv8_attn(q, lengths, table, k_codes, k_scales, v_codes, v_scales, softmax_scale, starts, out, out_dtype, workspace)
+
+
+# ---- low-rank adapters ---------------------------------------------------------------------------
+def lowrank_workspace_bytes(M, N, K, r):
+    return int(lib().rcp_lowrank_workspace_bytes(M, N, K, r))
+
+
+def lowrank_add(x, A, B, which, scaling, base, out=None, workspace=None):
+    """out[m] = base[m] + scaling[a] (x[m] A[a]^T) B[a]^T with a = which[m] (int32, outside the adapters: base alone).  x [M, K], A [adapters, r, K]
+    and B [adapters, N, r] float16 or bfloat16; base and out [M, N] (out may be base)."""
+    return _host.lowrank_add(x, A, B, which, scaling, base, out, workspace)

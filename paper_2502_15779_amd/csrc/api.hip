@@ -727,4 +727,167 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
                            softmax_scale, out, out_dtype, workspace, static_cast<hipStream_t>(stream));
 }
 
+// ---- paged 8-bit cache ----
+static bool any_dtype(rcp_dtype t) { return t == RCP_F16 || t == RCP_BF16 || t == RCP_F32; }
+
+static int check_kv8(const char* fn, const rcp_kv8_cache* c, const rcp_kv8_batch* b)
+{
+    if (!c || !b || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales || !b->lengths || !b->table)
+        return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
+    if (c->D != 64 && c->D != 128) return fail(RCP_ERR_UNSUPPORTED, "%s: D=%d (64 and 128 supported)", fn, c->D);
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128)
+        return fail(RCP_ERR_UNSUPPORTED, "%s: pages of %d tokens (16, 32, 64 and 128 supported)", fn, c->page);
+    if (c->n_pages < 1 || c->H < 1 || c->H > 4096) return fail(RCP_ERR_SHAPE, "%s: n_pages=%d, H=%d out of range", fn, c->n_pages, c->H);
+    if (b->sequences < 1 || b->sequences > RCP_KV8_MAX_SEQUENCES)
+        return fail(RCP_ERR_SHAPE, "%s: %d sequences (1 .. %d supported)", fn, b->sequences, RCP_KV8_MAX_SEQUENCES);
+    if (b->rows < 0 || b->rows > RCP_KV8_MAX_ROWS) return fail(RCP_ERR_SHAPE, "%s: %d rows (at most %d)", fn, b->rows, RCP_KV8_MAX_ROWS);
+    if (b->starts_or_null == nullptr && b->rows != b->sequences)
+        return fail(RCP_ERR_SHAPE, "%s: %d rows for %d sequences of one new token each", fn, b->rows, b->sequences);
+    if (b->width < 1 || static_cast<long long>(b->width) * c->page > (1 << 24) ||
+        static_cast<long long>(b->width) * c->page * b->sequences > 0x7fffffffLL)
+        return fail(RCP_ERR_SHAPE, "%s: a table of %d x %d pages of %d tokens", fn, b->sequences, b->width, c->page);
+    if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales) || !aligned16(b->lengths) ||
+        !aligned16(b->table) || !aligned16(b->starts_or_null))
+        return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);
+    return RCP_OK;
+}
+
+static int shift_of(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
+
+int rcp_kv8_append(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   rcp_dtype x_dtype, const float* rope_or_null, int rotate, const void* q_or_null, int64_t q_stride, int H_q,
+                   void* q_out_or_null, void* stream)
+{
+    const char* const fn = "rcp_kv8_append";
+    if (int rc = check_kv8(fn, cache, batch)) return rc;
+    if (batch->rows == 0) return RCP_OK;
+    if (!k || !v || (q_or_null && !q_out_or_null)) return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
+    if (!any_dtype(x_dtype)) return fail(RCP_ERR_UNSUPPORTED, "%s: unknown x_dtype %d", fn, static_cast<int>(x_dtype));
+    const bool several = batch->rows > 1;
+    auto stride_fits = [&](int64_t s, int heads) { return s % 8 == 0 && (!several || s >= static_cast<int64_t>(heads) * cache->D) && s <= (1LL << 31); };
+    if (!stride_fits(k_stride, cache->H) || !stride_fits(v_stride, cache->H) || (q_or_null && !stride_fits(q_stride, H_q)))
+        return fail(RCP_ERR_SHAPE, "%s: token strides must be multiples of 8 that hold a token's heads", fn);
+    if (q_or_null && (H_q < 1 || H_q > 4096)) return fail(RCP_ERR_SHAPE, "%s: H_q=%d out of range", fn, H_q);
+    const int shift = shift_of(cache->page);
+    const long long groups = 2LL * cache->H * ((batch->rows >> shift) + 2LL * batch->sequences) + 1;
+    if (groups + static_cast<long long>(batch->rows) * (q_or_null ? H_q : 0) > 0x7fffffffLL)
+        return fail(RCP_ERR_SHAPE, "%s: %d rows of %d and %d heads are too many", fn, batch->rows, cache->H, H_q);
+    if (!aligned16(k) || !aligned16(v) || !aligned16(q_or_null) || !aligned16(q_out_or_null) || !aligned16(rope_or_null))
+        return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);
+    Kv8AppendCall c = {};
+    c.k = k;
+    c.v = v;
+    c.q = q_or_null;
+    c.q_out = q_out_or_null;
+    c.k_stride = k_stride;
+    c.v_stride = v_stride;
+    c.q_stride = q_stride;
+    c.dtype = x_dtype;
+    c.rope = rope_or_null;
+    c.starts = batch->starts_or_null;
+    c.lengths = batch->lengths;
+    c.table = batch->table;
+    c.rows = batch->rows;
+    c.sequences = batch->sequences;
+    c.width = batch->width;
+    c.shift = shift;
+    c.n_pages = cache->n_pages;
+    c.H = cache->H;
+    c.H_q = H_q;
+    c.D = cache->D;
+    c.rotate = rotate != 0;
+    c.k_codes = cache->k_codes;
+    c.v_codes = cache->v_codes;
+    c.k_scales = cache->k_scales;
+    c.v_scales = cache->v_scales;
+    return launch_kv8_append(c, static_cast<hipStream_t>(stream));
+}
+
+size_t rcp_kv8_workspace_bytes(int rows, int sequences, int H_q, int H, int D, int one_token_each)
+{
+    if (rows < 0 || rows > RCP_KV8_MAX_ROWS || sequences < 1 || sequences > RCP_KV8_MAX_SEQUENCES || H < 1 || H_q < H || H_q > 4096 || H_q % H != 0 ||
+        (D != 64 && D != 128))
+        return 0;
+    return kv8_workspace_bytes(rows, sequences, H_q, H, D, one_token_each != 0);
+}
+
+int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const void* q, rcp_dtype q_dtype, int H_q, float softmax_scale,
+                 void* out, rcp_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const char* const fn = "rcp_kv8_attn";
+    if (int rc = check_kv8(fn, cache, batch)) return rc;
+    if (H_q < 1 || H_q > 4096 || H_q % cache->H != 0)
+        return fail(RCP_ERR_SHAPE, "%s: H_q=%d must be a positive multiple of H=%d, at most 4096", fn, H_q, cache->H);
+    if (!any_dtype(q_dtype) || !any_dtype(out_dtype))
+        return fail(RCP_ERR_UNSUPPORTED, "%s: unknown dtype (q %d, out %d)", fn, static_cast<int>(q_dtype), static_cast<int>(out_dtype));
+    if (batch->rows == 0) return RCP_OK;
+    if (!q || !out) return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);
+    const bool one = batch->starts_or_null == nullptr;
+    if ((static_cast<long long>(batch->rows) * (H_q / cache->H) / 128 + batch->sequences) * cache->H > 0x7fffffffLL / 32)
+        return fail(RCP_ERR_SHAPE, "%s: %d rows of %d heads are too many", fn, batch->rows, H_q);
+    const size_t need = kv8_workspace_bytes(batch->rows, batch->sequences, H_q, cache->H, cache->D, one);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(RCP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : static_cast<size_t>(0));
+    Kv8AttnCall c = {};
+    c.q = q;
+    c.q_dtype = q_dtype;
+    c.out_dtype = out_dtype;
+    c.starts = batch->starts_or_null;
+    c.lengths = batch->lengths;
+    c.table = batch->table;
+    c.rows = batch->rows;
+    c.sequences = batch->sequences;
+    c.width = batch->width;
+    c.shift = shift_of(cache->page);
+    c.n_pages = cache->n_pages;
+    c.H_q = H_q;
+    c.H_kv = cache->H;
+    c.D = cache->D;
+    c.k_codes = cache->k_codes;
+    c.v_codes = cache->v_codes;
+    c.k_scales = cache->k_scales;
+    c.v_scales = cache->v_scales;
+    c.softmax_scale = softmax_scale;
+    c.out = out;
+    c.workspace = workspace;
+    return launch_kv8_attn(c, static_cast<hipStream_t>(stream));
+}
+
+// ---- low-rank adapters ----
+static int check_lowrank(const char* fn, int M, int N, int K, int r)
+{
+    if (M < 0 || M > RCP_LOWRANK_MAX_M) return fail(RCP_ERR_SHAPE, "%s: M=%d outside 0..%d", fn, M, RCP_LOWRANK_MAX_M);
+    if (N < 1 || N % 4 != 0 || N > (1 << 24)) return fail(RCP_ERR_SHAPE, "%s: N=%d must be a positive multiple of 4", fn, N);
+    if (K < 1 || K % 32 != 0 || K > (1 << 24)) return fail(RCP_ERR_SHAPE, "%s: K=%d must be a positive multiple of 32", fn, K);
+    if (r < 1 || r % 8 != 0 || r > RCP_LOWRANK_MAX_R)
+        return fail(RCP_ERR_SHAPE, "%s: r=%d must be a positive multiple of 8, at most %d", fn, r, RCP_LOWRANK_MAX_R);
+    return RCP_OK;
+}
+
+size_t rcp_lowrank_workspace_bytes(int M, int N, int K, int r)
+{
+    if (check_lowrank("rcp_lowrank_workspace_bytes", M, N, K, r) != RCP_OK || M == 0) return 0;
+    return lowrank_workspace_bytes(M, N, K, r);
+}
+
+int rcp_lowrank_add(const void* x, rcp_dtype x_dtype, int M, int N, int K, int r, int adapters, const void* A, const void* B, const int32_t* which,
+                    const float* scaling, const void* base, void* out, rcp_dtype out_dtype, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const char* const fn = "rcp_lowrank_add";
+    if (int rc = check_lowrank(fn, M, N, K, r)) return rc;
+    if (adapters < 1) return fail(RCP_ERR_SHAPE, "%s: %d adapters", fn, adapters);
+    if (x_dtype != RCP_F16 && x_dtype != RCP_BF16) return fail(RCP_ERR_UNSUPPORTED, "%s: x_dtype must be RCP_F16 or RCP_BF16", fn);
+    if (!any_dtype(out_dtype)) return fail(RCP_ERR_UNSUPPORTED, "%s: unknown out_dtype %d", fn, static_cast<int>(out_dtype));
+    if (M == 0) return RCP_OK;
+    if (!x || !A || !B || !which || !scaling || !base || !out) return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
+    if (!aligned16(x) || !aligned16(A) || !aligned16(B) || !aligned16(which) || !aligned16(scaling) || !aligned16(base) || !aligned16(out) ||
+        !aligned16(workspace))
+        return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);
+    const size_t need = lowrank_workspace_bytes(M, N, K, r);
+    if (workspace == nullptr || workspace_bytes < need)
+        return fail(RCP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", fn, need, workspace ? workspace_bytes : static_cast<size_t>(0));
+    return launch_lowrank(x, x_dtype, M, N, K, r, adapters, A, B, which, scaling, base, out, out_dtype, workspace, static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <ATen/ops/zeros.h>
 #include <c10/core/DefaultDtype.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
@@ -742,6 +743,198 @@ PyObject* kv4_attn_decode_batched(Args a)
     return out.give();
 }
 
+// ---- paged 8-bit KV cache ---------------------------------------------------------------------------------
+// These calls read lengths and tables on the device, so that a tensor elsewhere would be an address that means nothing there.
+inline void same_device(const Tensor& t, const Tensor& as, const char* what)
+{
+    if (__builtin_expect(t.device() != as.device(), 0)) throw Bad{std::string(what) + " must be on the device of the first tensor"};
+}
+
+inline void on_current_device(const Tensor& t)
+{
+    require(t.is_cuda() && t.device().index() == c10::hip::current_device(), "the tensors must be on the current CUDA device");
+}
+
+inline const int32_t* whole_numbers(PyObject* o, const Tensor& as, int64_t count, const char* what)
+{
+    const Tensor& t = tensor(o, what);
+    if (t.scalar_type() != at::kInt || t.numel() != count) throw Bad{std::string(what) + " must be int32 of the documented size"};
+    same_device(t, as, what);
+    return static_cast<const int32_t*>(dev(t, what));
+}
+
+// k_codes, k_scales, v_codes, v_scales
+inline rcp_kv8_cache pages(Args a, const Tensor& as)
+{
+    const char* const message = "codes must be float8_e4m3fn [n_pages, H, page, D] and scales float32 [n_pages, H], contiguous, alike for keys and values";
+    const Tensor &kc = tensor(a[0], "k_codes"), &ks = tensor(a[1], "k_scales"), &vc = tensor(a[2], "v_codes"), &vs = tensor(a[3], "v_scales");
+    require(kc.scalar_type() == at::kFloat8_e4m3fn && vc.scalar_type() == at::kFloat8_e4m3fn && ks.scalar_type() == at::kFloat && vs.scalar_type() == at::kFloat &&
+                kc.dim() == 4 && ks.dim() == 2 && vc.sizes() == kc.sizes() && vs.sizes() == ks.sizes() && ks.size(0) == kc.size(0) && ks.size(1) == kc.size(1) &&
+                kc.is_contiguous() && ks.is_contiguous() && vc.is_contiguous() && vs.is_contiguous(),
+            message);
+    same_device(kc, as, "k_codes");
+    same_device(ks, as, "k_scales");
+    same_device(vc, as, "v_codes");
+    same_device(vs, as, "v_scales");
+    rcp_kv8_cache c;
+    c.n_pages = narrow(kc.size(0));
+    c.H = narrow(kc.size(1));
+    c.page = narrow(kc.size(2));
+    c.D = narrow(kc.size(3));
+    c.k_codes = dev(kc, "k_codes");
+    c.k_scales = static_cast<float*>(dev(ks, "k_scales"));
+    c.v_codes = dev(vc, "v_codes");
+    c.v_scales = static_cast<float*>(dev(vs, "v_scales"));
+    return c;
+}
+
+// lengths, table, starts or None
+inline rcp_kv8_batch batch(PyObject* lengths, PyObject* table, PyObject* starts, const Tensor& as)
+{
+    const Tensor &n = tensor(lengths, "lengths"), &t = tensor(table, "table");
+    require(n.dim() == 1 && t.dim() == 2 && t.size(0) == n.size(0) && t.size(1) > 0, "lengths must be [sequences] and table [sequences, width]");
+    rcp_kv8_batch b;
+    b.rows = narrow(as.size(0));
+    b.sequences = narrow(n.size(0));
+    b.width = narrow(t.size(1));
+    b.lengths = whole_numbers(lengths, as, n.size(0), "lengths");
+    b.table = whole_numbers(table, as, t.numel(), "table");
+    b.starts_or_null = none(starts) ? nullptr : whole_numbers(starts, as, n.size(0) + 1, "starts");
+    require(b.starts_or_null != nullptr || b.rows == b.sequences, "without starts there is one new token for each sequence");
+    return b;
+}
+
+// A tensor [rows, heads, D] whose tokens may lie apart (a view of a projection's output): elements from one token to the next
+inline int64_t token_stride(const Tensor& t, int64_t heads, int64_t D, const char* what)
+{
+    if (t.dim() != 3 || t.size(1) != heads || t.size(2) != D || !t.is_cuda() || (t.size(0) > 0 && D > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != D))
+        throw Bad{std::string(what) + " must be a CUDA tensor [rows, heads, D] with each token's heads side by side"};
+    return t.size(0) > 1 ? t.stride(0) : heads * D;
+}
+
+// k, v, lengths, table, k_codes, k_scales, v_codes, v_scales, starts, rope, rotate, q, q_out
+PyObject* kv8_append(Args a)
+{
+    const Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
+    const rcp_kv8_cache c = pages(a + 4, k);
+    const int64_t ks = token_stride(k, c.H, c.D, "k"), vs = token_stride(v, c.H, c.D, "v");
+    on_current_device(k);
+    require(v.size(0) == k.size(0) && v.scalar_type() == k.scalar_type(), "k and v must have as many tokens and one dtype");
+    same_device(v, k, "v");
+    const rcp_kv8_batch b = batch(a[2], a[3], a[8], k);
+    const rcp_dtype xd = in_dtype(k, "k and v must be float16, bfloat16 or float32");
+    const float* rope = nullptr;
+    if (!none(a[9])) {
+        const Tensor& r = tensor(a[9], "rope");
+        require(r.scalar_type() == at::kFloat && r.dim() == 2 && r.size(1) == c.D && r.size(0) >= static_cast<int64_t>(b.width) * c.page,
+                "rope must be float32 [positions, D] with a row for every position of the table (width * page)");
+        same_device(r, k, "rope");
+        rope = static_cast<const float*>(dev(r, "rope"));
+    }
+    const int rotate = truth(a[10]);
+    const void* q = nullptr;
+    int64_t qs = 0;
+    int H_q = 0;
+    Result q_out;
+    if (!none(a[11])) {
+        const Tensor& t = tensor(a[11], "q");
+        require(t.dim() == 3 && t.size(0) == k.size(0) && t.scalar_type() == k.scalar_type(), "q must be [rows, H_q, D] of k's dtype");
+        H_q = narrow(t.size(1));
+        qs = token_stride(t, H_q, c.D, "q");
+        same_device(t, k, "q");
+        if (!none(a[12])) q_out = given(a[12], "q_out");
+        // rows of no sequence are not written
+        else q_out.t = none(a[8]) ? empty_like_device({t.size(0), H_q, c.D}, t.scalar_type(), t) : at::zeros({t.size(0), H_q, c.D}, at::TensorOptions().dtype(t.scalar_type()).device(t.device()));
+        require(q_out.t.scalar_type() == t.scalar_type() && q_out.t.numel() == t.numel(), "q_out must be [rows, H_q, D] of q's dtype");
+        same_device(q_out.t, k, "q_out");
+        dev(q_out.t, "q_out");
+        q = t.data_ptr();
+    } else
+        require(none(a[12]), "q_out without q");
+    if (b.rows > 0) {
+        const void *const kp = k.data_ptr(), *const vp = v.data_ptr();
+        void* const o = q != nullptr ? q_out.t.data_ptr() : nullptr;
+        call([&](void* st) { return rcp_kv8_append(&c, &b, kp, ks, vp, vs, xd, rope, rotate, q, qs, H_q, o, st); });
+    }
+    return none(a[11]) ? nothing() : q_out.give();
+}
+
+// q, lengths, table, k_codes, k_scales, v_codes, v_scales, softmax_scale, starts, out, out_dtype, workspace
+PyObject* kv8_attn(Args a)
+{
+    const Tensor& q = tensor(a[0], "q");
+    const rcp_kv8_cache c = pages(a + 3, q);
+    require(q.dim() == 3 && q.size(2) == c.D, "q must be [rows, H_q, D]");
+    void* const qp = dev(q, "q");
+    on_current_device(q);
+    const rcp_kv8_batch b = batch(a[1], a[2], a[8], q);
+    const rcp_dtype qd = in_dtype(q, "q must be float16, bfloat16 or float32");
+    const int H_q = narrow(q.size(1));
+    const float scale = real(a[7]);
+    Result out;
+    if (!none(a[9])) out = given(a[9], "out");
+    else if (none(a[8])) out.t = empty_like_device(q.sizes(), scalar_type(a[10]), q);
+    else out.t = at::zeros(q.sizes(), at::TensorOptions().dtype(scalar_type(a[10])).device(q.device()));  // rows of no sequence are not written
+    const char* const fits = "out must be float16, bfloat16 or float32 [rows, H_q, D]";
+    const rcp_dtype od = in_dtype(out.t, fits);
+    require(out.t.numel() == q.numel(), fits);
+    same_device(out.t, q, "out");
+    void* const o = dev(out.t, "out");
+    if (b.rows == 0) return out.give();
+    Tensor work;
+    if (none(a[11])) {
+        const int64_t need = static_cast<int64_t>(rcp_kv8_workspace_bytes(b.rows, b.sequences, H_q, c.H, c.D, b.starts_or_null == nullptr));
+        work = empty_like_device({need > 16 ? need : 16}, at::kByte, q);
+    } else
+        work = tensor(a[11], "workspace");
+    same_device(work, q, "workspace");
+    void* const ws = dev(work, "workspace");
+    call([&](void* st) { return rcp_kv8_attn(&c, &b, qp, qd, H_q, scale, o, od, ws, work.nbytes(), st); });
+    return out.give();
+}
+
+// ---- low-rank adapters ------------------------------------------------------------------------------------
+// x, A, B, which, scaling, base, out, workspace
+PyObject* lowrank_add(Args a)
+{
+    const Tensor &x = tensor(a[0], "x"), &A = tensor(a[1], "A"), &B = tensor(a[2], "B"), &base = tensor(a[5], "base"), &s = tensor(a[4], "scaling");
+    require(x.dim() == 2 && (x.scalar_type() == at::kHalf || x.scalar_type() == at::kBFloat16), "x must be float16 or bfloat16 [M, K]");
+    require(A.dim() == 3 && B.dim() == 3 && A.scalar_type() == x.scalar_type() && B.scalar_type() == x.scalar_type() && A.size(0) == B.size(0) &&
+                A.size(1) == B.size(2) && A.size(2) == x.size(1),
+            "A must be [adapters, r, K] and B [adapters, N, r] of x's dtype");
+    const char* const fits = "base and out must be float16, bfloat16 or float32 [M, N] of one dtype";
+    require(base.dim() == 2 && base.size(0) == x.size(0) && base.size(1) == B.size(1), fits);
+    const rcp_dtype xd = in_dtype(x, fits), od = in_dtype(base, fits);
+    require(s.scalar_type() == at::kFloat && s.numel() == A.size(0), "scaling must be float32 [adapters]");
+    void *const xp = dev(x, "x"), *const Ap = dev(A, "A"), *const Bp = dev(B, "B"), *const bp = dev(base, "base"), *const sp = dev(s, "scaling");
+    on_current_device(x);
+    same_device(A, x, "A");
+    same_device(B, x, "B");
+    same_device(base, x, "base");
+    same_device(s, x, "scaling");
+    const int32_t* const which = whole_numbers(a[3], x, x.size(0), "which");
+    Result out;
+    if (none(a[6])) out.t = empty_like_device(base.sizes(), base.scalar_type(), base);
+    else out = given(a[6], "out");
+    require(out.t.scalar_type() == base.scalar_type() && out.t.numel() == base.numel(), fits);
+    same_device(out.t, x, "out");
+    void* const o = dev(out.t, "out");
+    const int M = narrow(x.size(0)), K = narrow(x.size(1)), N = narrow(B.size(1)), r = narrow(A.size(1)), adapters = narrow(A.size(0));
+    if (M == 0) return out.give();
+    Tensor work;
+    if (none(a[7])) {
+        const int64_t need = static_cast<int64_t>(rcp_lowrank_workspace_bytes(M, N, K, r));
+        work = empty_like_device({need > 16 ? need : 16}, at::kByte, x);
+    } else
+        work = tensor(a[7], "workspace");
+    same_device(work, x, "workspace");
+    void* const ws = dev(work, "workspace");
+    call([&](void* st) {
+        return rcp_lowrank_add(xp, xd, M, N, K, r, adapters, Ap, Bp, which, static_cast<const float*>(sp), bp, o, od, ws, work.nbytes(), st);
+    });
+    return out.give();
+}
+
 // ---- module ---------------------------------------------------------------------------------------------
 template <PyObject* (*F)(Args), int COUNT>
 PyObject* entry(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -796,6 +989,9 @@ PyMethodDef g_methods[] = {
     RCP_ENTRY(kv4_attn_decode, 11),
     RCP_ENTRY(kv4_append_batched, 6),
     RCP_ENTRY(kv4_attn_decode_batched, 10),
+    RCP_ENTRY(kv8_append, 13),
+    RCP_ENTRY(kv8_attn, 12),
+    RCP_ENTRY(lowrank_add, 8),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -1,0 +1,699 @@
+// Attention over the paged 8-bit cache.
+//
+//   out_r = sum_t 2^(score_rt) V_t / sum_t 2^(score_rt),   score_rt = log2(e) softmax_scale s_t (q_r . c_t),   V_t = s'_t c'_t
+// over the tokens t that row r (a new token's query head) may see; c, c' are the E4M3 codes of a token, s, s' the scales of its page.
+//
+// Both products run transposed on the matrix cores: scores as (tokens x rows) = codes x queries, outputs as (elements x rows) = value
+// codes transposed x weights.  A lane of a result then holds one row and several tokens, which is how the second product takes its weights:
+// they stay in registers, and a row's maximum, sum and correction are values of its lanes.  The order of the products' inner index is
+// free as long as both operands share it, so that keys enter in 16-byte pieces as they lie in memory and values in the tokens that a
+// lane has weights of; value codes come back transposed from LDS (ds_read_b64_tr_b8: eight rows of sixteen bytes, a lane gets a column).
+// A code becomes a binary16 number, exactly, half an instruction each.
+//
+// The query of a row is scaled by a power of two that puts its largest element at 2^13 .. 2^14: one binary16 number holds a 16-bit
+// query exactly down to 2^-28 of that; a binary32 query takes two (QP).  Weights are 2^(score - m) s' <= 2^14 in one binary16 number where the result has no
+// more than 8 or 11 bits itself, in two otherwise (PP); the reference m of a row is held against score + log2 s', so that a page of a large scale and
+// little attention does not push the others out of binary16, and moves only when a weight would leave the range.  Sums are binary32.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kv8.hpp"
+
+namespace rcp {
+
+constexpr float KV8_LOG2E = 1.44269504088896340736f;
+constexpr float KV8_LOW = -3.0e38f;    // a reference that no score has raised yet (finite: differences with it stay numbers)
+constexpr float KV8_TOP = 14.0f, KV8_REF = 9.0f;  // weights stay below 2^14; a raised reference puts the largest so far at 2^9
+constexpr int KV8_TILE = 64;           // tokens a step
+constexpr int KV8_EXTRA = 4;           // floats behind the D sums of a partial result: m, l
+
+struct Kv8AttnArgs {
+    Kv8Table t;
+    const void* q;
+    int q_dt, out_dt, rows, H_q, H_kv, rep;
+    float softmax_scale;
+    const unsigned char *k_codes, *v_codes;
+    const float *k_scales, *v_scales;
+    void* out;
+    float* part;
+    int chunks;   // one token a sequence: chunks of the grid; otherwise splits of the cached tokens
+    int tiles;    // several tokens: tiles of rows in the grid
+};
+
+__device__ __forceinline__ v8h kv8_halves(uint32_t a, uint32_t b)
+{
+    const v2h w = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
+    const v2h y = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), z = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
+    return v8h{w[0], w[1], x[0], x[1], y[0], y[1], z[0], z[1]};
+}
+
+// eight numbers as binary16, and what that leaves of them
+__device__ __forceinline__ v8h kv8_round(const float (&v)[8])
+{
+    v8h h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e]);
+    return h;
+}
+__device__ __forceinline__ v8h kv8_rest(const float (&v)[8], const v8h& h)
+{
+    v8h r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = static_cast<_Float16>(v[e] - static_cast<float>(h[e]));
+    return r;
+}
+
+// eight query elements from index i on
+__device__ __forceinline__ void kv8_query8(const Kv8AttnArgs& a, size_t i, float (&v)[8])
+{
+    if (a.q_dt == RCP_F32) load8_as_float<RCP_F32>(a.q, i, v);  // uniform
+    else if (a.q_dt == RCP_F16) load8_as_float<RCP_F16>(a.q, i, v);
+    else load8_as_float<RCP_BF16>(a.q, i, v);
+}
+
+__device__ __forceinline__ float kv8_swap32_max(float v)
+{
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float kv8_swap16_max(float v)
+{
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ void kv8_put(void* out, int dt, size_t i, float v)
+{
+    if (dt == RCP_F32) static_cast<float*>(out)[i] = v;  // uniform
+    else if (dt == RCP_F16) static_cast<__half*>(out)[i] = round_to_half(v);
+    else static_cast<__bf16*>(out)[i] = static_cast<__bf16>(v);
+}
+
+// log2 of a page's scale as the weights' reference takes it: scales are 2^-40 .. 2^120, and a page that was never written has 0
+__device__ __forceinline__ float kv8_log_scale(float s) { return __builtin_amdgcn_logf(__builtin_amdgcn_fmed3f(s, 0x1p-40f, 0x1p120f)); }
+
+// the page that holds position `pos` of sequence b, -1 where there is none
+__device__ __forceinline__ int kv8_page(const Kv8Table& t, const int* row, int pos)
+{
+    const int id = row[min(pos >> t.shift, t.width - 1)];
+    return pos < t.capacity && static_cast<unsigned>(id) < static_cast<unsigned>(t.n_pages) ? id : -1;
+}
+
+// Sixteen consecutive cached tokens of a head, whose page is `id`, as a buffer that ends with the last of them below `end`: beyond, and without a
+// page, reads give zero.
+struct Kv8Block {
+    size_t at;  // first token, in tokens of the pool
+    int tokens;
+};
+__device__ __forceinline__ Kv8Block kv8_block(const Kv8Table& t, int H, int h, int id, int pos, int end)
+{
+    return {((static_cast<size_t>(max(id, 0)) * H + h) << t.shift) + (pos & ((1 << t.shift) - 1)), id < 0 ? 0 : kv8_clamp(end - pos, 0, 16)};
+}
+
+// 16 bytes of a lane from a buffer straight into LDS, lane after lane from `to` on (a function of its own: inside a template, the host's
+// pass drops the kernel over it)
+__device__ __forceinline__ void kv8_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* to, int offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+}
+__device__ __forceinline__ void kv8_to_lds_once(__amdgpu_buffer_rsrc_t from, unsigned char* to, int offset)  // read once per call: non-temporal
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 2);
+}
+
+// ---------------------------------------------------------------------------------------
+// One new token a sequence.  Workgroup = (chunk of cached tokens of a sequence, cache head [, sixteen of its query heads]); the chunks are cut on
+// the device from the lengths, so that a captured call stays balanced when they change.  Wavefront w of the four walks the tiles
+// w, w + 4, ... of 64 tokens on its own.  16x16x32 products: a lane holds the row (query head) lane % 16.
+// ---------------------------------------------------------------------------------------
+template <int D>
+struct Kv8DecodeLds {
+    union {
+        unsigned char v[4][KV8_TILE * D];  // a tile's value codes of each wavefront
+        float red[4][16][D];
+    };
+    float m[4][16], l[4][16];
+};
+
+// which 16-byte piece of a token's value codes stands at place p of its row in LDS: p ^ this; the rows that a transposing read takes together
+// (tokens 4g .. 4g + 3 and sixteen further, for two g at a time) fall into different banks
+template <int D>
+__device__ __forceinline__ int kv8_decode_swizzle(int token)
+{
+    if constexpr (D == 128) return ((token >> 1) & 1) | ((token >> 3) & 2) | (token & 4);
+    else return ((token >> 4) & 1) | ((token >> 1) & 2);
+}
+
+template <int D, int QP, int PP>
+__global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
+{
+    constexpr int KX = D / 64;  // 16-byte loads of a lane for sixteen tokens' keys
+    __shared__ Kv8DecodeLds<D> lds;
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int chunk = static_cast<int>(blockIdx.x) / a.H_kv, hk = static_cast<int>(blockIdx.x) - chunk * a.H_kv;
+    auto length_of = [&](int b) { return kv8_clamp(a.t.lengths[b], 0, a.t.capacity); };
+    const int total = kv8_total(a.t.sequences, lane, length_of);
+    const int C = kv8_chunk_tokens(total, a.t.sequences, a.chunks, KV8_TILE);
+    const Kv8Unit u = kv8_find(a.t.sequences, chunk, lane, [&](int b) { return kv8_chunks(length_of(b), C); });
+    if (u.b < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(u.b), t0 = __builtin_amdgcn_readfirstlane(u.within) * C;
+    const int len = __builtin_amdgcn_readfirstlane(length_of(b)), t_end = min(len, t0 + C);
+    const int R = min(16, a.rep - static_cast<int>(blockIdx.y) * 16);
+    const int h0 = hk * a.rep + static_cast<int>(blockIdx.y) * 16;
+    const int first = t0 + KV8_TILE * wave;
+    const int tiles = t_end > first ? (t_end - first + 4 * KV8_TILE - 1) / (4 * KV8_TILE) : 0;
+    const int* const row = a.t.table + static_cast<size_t>(b) * a.t.width;
+
+    // ---- the query: lane = (head i, the elements of the key pieces 16 g .. of each 64) ----
+    v8h qh[2 * KX], ql[QP == 2 ? 2 * KX : 1];
+    float unit;
+    {
+        float t[2 * KX][8];
+        const size_t at = (static_cast<size_t>(b) * a.H_q + h0 + min(i, R - 1)) * D + 16 * g;
+        float top = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 2 * KX; ++d) kv8_query8(a, at + 64 * (d >> 1) + 8 * (d & 1), t[d]);
+#pragma unroll
+        for (int d = 0; d < 2 * KX; ++d)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(t[d][e]));
+        top = kv8_swap32_max(kv8_swap16_max(top));
+        const int E = __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+        for (int d = 0; d < 2 * KX; ++d) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[d][e] = ldexpf(t[d][e], 14 - E);
+            qh[d] = kv8_round(t[d]);
+            if constexpr (QP == 2) ql[d] = kv8_rest(t[d], qh[d]);
+        }
+        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
+    }
+
+    auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
+    };
+    u32x4 kw[4][KX];
+    float ks[4], vs[4];
+    bool page[4];
+    auto load_tile = [&](int base) {  // keys into registers, values into LDS
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const int pos = base + 16 * n;
+            const int id = __builtin_amdgcn_readfirstlane(pos < t_end ? kv8_page(a.t, row, pos) : -1);
+            page[n] = id >= 0;
+            const size_t s = static_cast<size_t>(max(id, 0)) * a.H_kv + hk;
+            ks[n] = a.k_scales[s];
+            vs[n] = a.v_scales[s];
+            const Kv8Block block = kv8_block(a.t, a.H_kv, hk, id, pos, t_end);
+            const __amdgpu_buffer_rsrc_t kr = resource(a.k_codes, block), vr = resource(a.v_codes, block);
+#pragma unroll
+            for (int x = 0; x < KX; ++x) kw[n][x] = __builtin_amdgcn_raw_buffer_load_b128(kr, i * D + 16 * g + 64 * x, 0, 2);
+#pragma unroll
+            for (int y = 0; y < KX; ++y) {
+                constexpr int P = D / 16;  // pieces a token
+                const int s16 = 64 * y + lane, token = s16 / P, at = s16 % P;
+                kv8_to_lds_once(vr, &lds.v[wave][16 * n * D + 1024 * y], token * D + ((at ^ kv8_decode_swizzle<D>(16 * n + token)) * 16));
+            }
+        }
+    };
+
+    v4f acc[D / 16];
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) acc[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = KV8_LOW, l = 0.0f;
+    for (int c = 0; c < tiles; ++c) {
+        const int base = first + 4 * KV8_TILE * c;
+        load_tile(base);
+        v4f S[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            S[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int d = 0; d < 2 * KX; ++d) {
+                const v8h k = kv8_halves(kw[n][d >> 1][2 * (d & 1)], kw[n][d >> 1][2 * (d & 1) + 1]);
+                if constexpr (QP == 2) S[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, ql[d], S[n], 0, 0, 0);
+                S[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qh[d], S[n], 0, 0, 0);
+            }
+        }
+        float sc[4][4], top = -INFINITY;
+        const bool whole = base + KV8_TILE <= t_end && page[0] && page[1] && page[2] && page[3];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const float by = ks[n] * unit;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[n][j] = S[n][j] * by;
+            if (!whole) {  // uniform
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[n][j] = page[n] && base + 16 * n + 4 * g + j < t_end ? sc[n][j] : -INFINITY;
+            }
+            top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])) + kv8_log_scale(vs[n]));
+        }
+        if (__builtin_amdgcn_ballot_w64(top > m + KV8_TOP) != 0) {
+            const float t = kv8_swap32_max(kv8_swap16_max(top));
+            const float m_new = t > m + KV8_TOP ? t - KV8_REF : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) acc[d] *= alpha;
+        }
+        v8h ph[2], pl[PP == 2 ? 2 : 1];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int n = 2 * s + (e >> 2);
+                const float p = __builtin_amdgcn_exp2f(sc[n][e & 3] - m);
+                l += p;
+                w[e] = p * vs[n];
+            }
+            ph[s] = kv8_round(w);
+            if constexpr (PP == 2) pl[s] = kv8_rest(w, ph[s]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // the values are in LDS
+        __builtin_amdgcn_sched_barrier(0);
+        const int r = i >> 1;
+        const int token = 16 * (r >> 2) + 4 * g + (r & 3);
+        const unsigned char* const at = &lds.v[wave][0] + token * D + (i & 1) * 8;
+        const int f = kv8_decode_swizzle<D>(token);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (__attribute__((address_space(3))) v2i*)(at + 32 * s * D + ((d ^ f) * 16)));
+                const v8h v = kv8_halves(static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]));
+                if constexpr (PP == 2) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[s], acc[d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[s], acc[d], 0, 0, 0);
+            }
+        // every read of the tile has returned before the next one overwrites it
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    l = fold32f(fold16f(l, l), fold16f(l, l));
+    __syncthreads();  // LDS changes hands
+    if (i < R) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<v4f*>(&lds.red[wave][i][16 * d + 4 * g]) = acc[d];
+        if (g == 0) {
+            lds.m[wave][i] = m;
+            lds.l[wave][i] = l;
+        }
+    }
+    __syncthreads();
+    const bool alone = kv8_chunks(len, C) == 1;
+    for (int idx = tid; idx < R * D; idx += 256) {
+        const int h = idx / D, j = idx % D;
+        float M = lds.m[0][h];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) M = fmaxf(M, lds.m[w][h]);
+        float sum = 0.0f, ls = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float e = __builtin_amdgcn_exp2f(lds.m[w][h] - M);
+            sum = fmaf(e, lds.red[w][h][j], sum);
+            ls = fmaf(e, lds.l[w][h], ls);
+        }
+        if (alone) kv8_put(a.out, a.out_dt, (static_cast<size_t>(b) * a.H_q + h0 + h) * D + j, ls == 0.0f ? 0.0f : sum / ls);
+        else {
+            float* const dst = a.part + (static_cast<size_t>(chunk) * a.H_q + h0 + h) * (D + KV8_EXTRA);
+            dst[j] = sum;
+            if (j == 0) {
+                dst[D] = M;
+                dst[D + 1] = ls;
+            }
+        }
+    }
+}
+
+// Merges n partial results `stride` floats apart into one row: thread (part, j) of `groups` x D takes every groups-th of them.
+template <int D>
+__device__ __forceinline__ void kv8_merge(const float* src, size_t stride, int n, void* out, int out_dt, size_t row)
+{
+    constexpr int GROUPS = 512 / D;
+    __shared__ float red[GROUPS][D], dred[GROUPS], mred[GROUPS];
+    const int j = threadIdx.x % D, g = threadIdx.x / D;
+    float M = KV8_LOW, num = 0.0f, den = 0.0f;
+    for (int i0 = g; i0 < n; i0 += 4 * GROUPS) {
+        float mi[4], li[4], ai[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float* const s = src + static_cast<size_t>(min(i0 + GROUPS * x, n - 1)) * stride;
+            mi[x] = s[D];
+            li[x] = s[D + 1];
+            ai[x] = s[j];
+        }
+        float mb = M;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (i0 + GROUPS * x < n) mb = fmaxf(mb, mi[x]);
+        const float r = __builtin_amdgcn_exp2f(M - mb);
+        num *= r;
+        den *= r;
+        M = mb;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const float e = i0 + GROUPS * x < n ? __builtin_amdgcn_exp2f(mi[x] - M) : 0.0f;
+            num = fmaf(e, ai[x], num);
+            den = fmaf(e, li[x], den);
+        }
+    }
+    red[g][j] = num;
+    if (j == 0) {
+        dred[g] = den;
+        mred[g] = M;
+    }
+    __syncthreads();
+    if (g == 0) {
+        float Mt = mred[0];
+#pragma unroll
+        for (int x = 1; x < GROUPS; ++x) Mt = fmaxf(Mt, mred[x]);
+        num = den = 0.0f;
+#pragma unroll
+        for (int x = 0; x < GROUPS; ++x) {
+            const float e = __builtin_amdgcn_exp2f(mred[x] - Mt);
+            num = fmaf(e, red[x][j], num);
+            den = fmaf(e, dred[x], den);
+        }
+        kv8_put(out, out_dt, row * D + j, den == 0.0f ? 0.0f : num / den);
+    }
+}
+
+// blockIdx = (query head, sequence): the chunks of a sequence that has more than one
+template <int D>
+__global__ __launch_bounds__(512) void kv8_decode_merge_kernel(Kv8AttnArgs a)
+{
+    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63;
+    auto length_of = [&](int x) { return kv8_clamp(a.t.lengths[x], 0, a.t.capacity); };
+    const int C = kv8_chunk_tokens(kv8_total(a.t.sequences, lane, length_of), a.t.sequences, a.chunks, KV8_TILE);
+    const int n = kv8_chunks(length_of(b), C);
+    if (n == 1) return;  // the attention kernel has written it
+    const int before = kv8_total(b, lane, [&](int x) { return kv8_chunks(length_of(x), C); });
+    kv8_merge<D>(a.part + (static_cast<size_t>(before) * a.H_q + h) * (D + KV8_EXTRA), static_cast<size_t>(a.H_q) * (D + KV8_EXTRA), n, a.out, a.out_dt,
+                 static_cast<size_t>(b) * a.H_q + h);
+}
+
+// ---------------------------------------------------------------------------------------
+// Several new tokens a sequence, each of which sees the tokens up to its own.  Workgroup = (128 rows of a sequence and cache head, [part of
+// the cached tokens]); row = (new token, query head of the group).  32x32x16 products: a lane holds the row lane % 32 of its
+// wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS.
+// ---------------------------------------------------------------------------------------
+constexpr int KV8_ROWS = 128;
+
+template <int D>
+__device__ __forceinline__ int kv8_prompt_swizzle(int token)
+{
+    if constexpr (D == 128) return ((token >> 2) & 1) | (token & 2) | ((token >> 1) & 4);
+    else return ((token >> 2) & 1) | ((token >> 2) & 2);
+}
+
+template <int D, int QP, int PP>
+__global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
+{
+    constexpr int KL = D / 32, DB = D / 32, P = D / 16, LOADS = D / 64;
+    __shared__ unsigned char kt[2][KV8_TILE * D], vt[2][KV8_TILE * D];
+    __shared__ float4 info[2][4];  // of sixteen tokens: key scale, value scale, its logarithm, 1 where there is a page
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int rest = blockIdx.x;
+    const int hk = rest % a.H_kv;
+    rest /= a.H_kv;
+    const int split = rest % a.chunks, unit_of = a.tiles - 1 - rest / a.chunks;  // the last rows first: they see most
+    const Kv8Unit u = kv8_find(a.t.sequences, unit_of, lane, [&](int b) {
+        return static_cast<int>((static_cast<long long>(kv8_run(a.t.starts, a.t.lengths, b, a.rows).count) * a.rep + KV8_ROWS - 1) / KV8_ROWS);
+    });
+    if (u.b < 0) return;
+    const int b = __builtin_amdgcn_readfirstlane(u.b), row0 = __builtin_amdgcn_readfirstlane(u.within) * KV8_ROWS;
+    const Kv8Run run = kv8_run(a.t.starts, a.t.lengths, b, a.rows);
+    const int pos0 = __builtin_amdgcn_readfirstlane(run.pos), first = __builtin_amdgcn_readfirstlane(run.first);
+    const int n_rows = __builtin_amdgcn_readfirstlane(run.count) * a.rep;
+    const int len = min(__builtin_amdgcn_readfirstlane(run.length), a.t.capacity);
+    auto sees = [&](int r) { return kv8_clamp(pos0 + min(r, n_rows - 1) / a.rep + 1, 0, len); };  // tokens that row r may see
+    const int wg_sees = sees(row0 + KV8_ROWS - 1);
+    const int all_tiles = (wg_sees + KV8_TILE - 1) / KV8_TILE, per = (all_tiles + a.chunks - 1) / a.chunks;
+    const int tile0 = split * per, tile1 = min(all_tiles, tile0 + per);
+    const int my = row0 + 32 * wave + c, limit = sees(my);
+    const int wave_least = __builtin_amdgcn_readfirstlane(sees(row0 + 32 * wave)), wave_most = __builtin_amdgcn_readfirstlane(sees(row0 + 32 * wave + 31));
+    const int* const table = a.t.table + static_cast<size_t>(b) * a.t.width;
+    const int token = first + min(my, n_rows - 1) / a.rep, head = hk * a.rep + min(my, n_rows - 1) % a.rep;
+    const size_t out_row = static_cast<size_t>(token) * a.H_q + head;
+
+    v8h qh[KL][2], ql[QP == 2 ? KL : 1][2];
+    float unit;
+    {
+        float t[KL][2][8], top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KL; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                kv8_query8(a, out_row * D + 32 * k + 16 * hh + 8 * x, t[k][x]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(t[k][x][e]));
+            }
+        top = kv8_swap32_max(top);
+        const int E = __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+        for (int k = 0; k < KL; ++k)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], 14 - E);
+                qh[k][x] = kv8_round(t[k][x]);
+                if constexpr (QP == 2) ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
+            }
+        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
+    }
+
+    auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
+    };
+    auto stage = [&](int tile, int buf) {  // sixteen tokens of the tile by each wavefront
+        const int pos = tile * KV8_TILE + 16 * wave;
+        const int id = __builtin_amdgcn_readfirstlane(pos < wg_sees ? kv8_page(a.t, table, pos) : -1);
+        const Kv8Block block = kv8_block(a.t, a.H_kv, hk, id, pos, wg_sees);
+        const __amdgpu_buffer_rsrc_t kr = resource(a.k_codes, block), vr = resource(a.v_codes, block);
+#pragma unroll
+        for (int y = 0; y < LOADS; ++y) {
+            const int s16 = 64 * y + lane, tk = s16 / P, at = s16 % P;
+            const int from = tk * D + ((at ^ kv8_prompt_swizzle<D>(16 * wave + tk)) * 16);
+            kv8_to_lds(kr, &kt[buf][16 * wave * D + 1024 * y], from);
+            kv8_to_lds(vr, &vt[buf][16 * wave * D + 1024 * y], from);
+        }
+        const size_t s = static_cast<size_t>(max(id, 0)) * a.H_kv + hk;
+        const float vscale = a.v_scales[s];
+        if (lane == 0) info[buf][wave] = make_float4(a.k_scales[s], vscale, kv8_log_scale(vscale), id >= 0 ? 1.0f : 0.0f);
+    };
+
+    v16f acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
+    float m = KV8_LOW, l = 0.0f;
+    if (tile0 < tile1) stage(tile0, 0);
+    for (int tile = tile0; tile < tile1; ++tile) {
+        const int buf = (tile - tile0) & 1, base = tile * KV8_TILE;
+        __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the tile is in LDS,
+        __syncthreads();                // everybody's is, and the other buffer has been read
+        if (tile + 1 < tile1) stage(tile + 1, buf ^ 1);
+        if (base >= wave_most) continue;  // uniform over the wavefront: none of its rows sees the tile
+        v16f S[2];
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[tb][e] = 0.0f;
+            const int tk = 32 * tb + c;
+            const unsigned char* const at = &kt[buf][tk * D];
+            const int f = kv8_prompt_swizzle<D>(tk);
+#pragma unroll
+            for (int k = 0; k < KL; ++k) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(at + (((2 * k + hh) ^ f) * 16));
+                const v8h k0 = kv8_halves(w[0], w[1]), k1 = kv8_halves(w[2], w[3]);
+                if constexpr (QP == 2) {
+                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[k][0], S[tb], 0, 0, 0);
+                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[k][1], S[tb], 0, 0, 0);
+                }
+                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[k][0], S[tb], 0, 0, 0);
+                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k][1], S[tb], 0, 0, 0);
+            }
+        }
+        float4 page[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) page[n] = info[buf][n];
+        const bool whole = base + KV8_TILE <= wave_least && page[0].w + page[1].w + page[2].w + page[3].w == 4.0f;
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {  // sixteen tokens: eight scores of a lane
+            const float by = page[n].x * unit;
+            float most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = S[n >> 1][8 * (n & 1) + e] * by;
+                if (!whole) x = page[n].w != 0.0f && base + 16 * n + 8 * (e >> 2) + 4 * hh + (e & 3) < limit ? x : -INFINITY;
+                S[n >> 1][8 * (n & 1) + e] = x;
+                most = fmaxf(most, x);
+            }
+            top = fmaxf(top, most + page[n].z);
+        }
+        if (__builtin_amdgcn_ballot_w64(top > m + KV8_TOP) != 0) {
+            const float t = kv8_swap32_max(top);
+            const float m_new = t > m + KV8_TOP ? t - KV8_REF : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+        }
+        const int r = (lane & 15) >> 1;
+        const int vtok = 8 * (r >> 2) + 4 * hh + (r & 3), f = kv8_prompt_swizzle<D>(vtok), dhalf = (lane >> 4) & 1;
+        const unsigned char* const vat = &vt[buf][vtok * D + (lane & 1) * 8];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = __builtin_amdgcn_exp2f(S[n >> 1][8 * (n & 1) + e] - m);
+                l += p;
+                w[e] = p * page[n].y;
+            }
+            const v8h ph = kv8_round(w);
+            v8h pl;
+            if constexpr (PP == 2) pl = kv8_rest(w, ph);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (__attribute__((address_space(3))) v2i*)(vat + 16 * n * D + (((2 * d + dhalf) ^ f) * 16)));
+                const v8h v = kv8_halves(static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]));
+                if constexpr (PP == 2) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pl, acc[d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, ph, acc[d], 0, 0, 0);
+            }
+        }
+    }
+    l = fold32f(l, l);
+    if (my >= n_rows) return;
+    if (a.chunks == 1) {
+        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) kv8_put(a.out, a.out_dt, out_row * D + 32 * d + 8 * (e >> 2) + 4 * hh + (e & 3), l == 0.0f ? 0.0f : acc[d][e] * by);
+    } else {
+        float* const dst = a.part + (static_cast<size_t>(split) * a.rows * a.H_q + out_row) * (D + KV8_EXTRA);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4*>(dst + 32 * d + 8 * (e >> 2) + 4 * hh) = make_float4(acc[d][e], acc[d][e + 1], acc[d][e + 2], acc[d][e + 3]);
+        if (hh == 0) {
+            dst[D] = m;
+            dst[D + 1] = l;
+        }
+    }
+}
+
+// blockIdx = (query head, row of the call)
+template <int D>
+__global__ __launch_bounds__(512) void kv8_prompt_merge_kernel(Kv8AttnArgs a)
+{
+    const int h = blockIdx.x, t = blockIdx.y;
+    if (kv8_sequence_of(a.t.starts, a.t.sequences, t, a.rows) < 0) return;
+    const size_t row = static_cast<size_t>(t) * a.H_q + h, stride = static_cast<size_t>(a.rows) * a.H_q * (D + KV8_EXTRA);
+    kv8_merge<D>(a.part + row * (D + KV8_EXTRA), stride, a.chunks, a.out, a.out_dt, row);
+}
+
+// ---------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------
+struct Kv8AttnPlan {
+    int chunks, tiles;  // as in Kv8AttnArgs
+    size_t bytes;       // of partial results
+};
+
+static Kv8AttnPlan kv8_attn_plan(int rows, int sequences, int H_q, int H_kv, int D, bool one)
+{
+    Kv8AttnPlan p;
+    const int cus = num_compute_units(), rep = H_q / H_kv;
+    const size_t partial = static_cast<size_t>(H_q) * (D + KV8_EXTRA) * sizeof(float);
+    if (one) {
+        p.chunks = 4 * cus / H_kv > 2 * sequences ? 4 * cus / H_kv : 2 * sequences;
+        p.tiles = 0;
+        p.bytes = static_cast<size_t>(p.chunks) * partial;
+    } else {
+        p.tiles = static_cast<int>(static_cast<long long>(rows) * rep / KV8_ROWS) + sequences;
+        const long long groups = static_cast<long long>(p.tiles) * H_kv;
+        p.chunks = 1;
+        if (groups < 2 * cus) {
+            const long long want = (2 * cus + groups - 1) / groups;
+            p.chunks = static_cast<int>(want < 32 ? want : 32);
+        }
+        p.bytes = p.chunks == 1 ? 0 : static_cast<size_t>(p.chunks) * rows * partial;
+    }
+    return p;
+}
+
+size_t kv8_workspace_bytes(int rows, int sequences, int H_q, int H_kv, int D, bool one)
+{
+    const size_t bytes = kv8_attn_plan(rows, sequences, H_q, H_kv, D, one).bytes;
+    return bytes > 16 ? bytes : 16;
+}
+
+int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
+{
+    const bool one = c.starts == nullptr;
+    const Kv8AttnPlan plan = kv8_attn_plan(c.rows, c.sequences, c.H_q, c.H_kv, c.D, one);
+    Kv8AttnArgs a;
+    a.t = {c.starts, c.lengths, c.table, c.sequences, c.width, c.shift, c.n_pages, c.width << c.shift};
+    a.q = c.q;
+    a.q_dt = c.q_dtype;
+    a.out_dt = c.out_dtype;
+    a.rows = c.rows;
+    a.H_q = c.H_q;
+    a.H_kv = c.H_kv;
+    a.rep = c.H_q / c.H_kv;
+    a.softmax_scale = c.softmax_scale;
+    a.k_codes = static_cast<const unsigned char*>(c.k_codes);
+    a.v_codes = static_cast<const unsigned char*>(c.v_codes);
+    a.k_scales = c.k_scales;
+    a.v_scales = c.v_scales;
+    a.out = c.out;
+    a.part = static_cast<float*>(c.workspace);
+    a.chunks = plan.chunks;
+    a.tiles = plan.tiles;
+    const bool q2 = c.q_dtype == RCP_F32;
+    auto form = [&](auto size) {
+        constexpr int D = decltype(size)::value;
+        if (one) {
+            const dim3 grid(static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv), static_cast<unsigned>((a.rep + 15) / 16));
+            auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
+            const bool p2 = c.out_dtype != RCP_BF16;
+            if (q2 && p2) launch(&kv8_decode_kernel<D, 2, 2>);
+            else if (q2) launch(&kv8_decode_kernel<D, 2, 1>);
+            else if (p2) launch(&kv8_decode_kernel<D, 1, 2>);
+            else launch(&kv8_decode_kernel<D, 1, 1>);
+        } else {
+            const unsigned grid = static_cast<unsigned>(plan.tiles) * static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv);
+            auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
+            const bool p2 = c.out_dtype == RCP_F32;
+            if (q2 && p2) launch(&kv8_prompt_kernel<D, 2, 2>);
+            else if (q2) launch(&kv8_prompt_kernel<D, 2, 1>);
+            else if (p2) launch(&kv8_prompt_kernel<D, 1, 2>);
+            else launch(&kv8_prompt_kernel<D, 1, 1>);
+        }
+    };
+    if (c.D == 128) form(std::integral_constant<int, 128>{});
+    else form(std::integral_constant<int, 64>{});
+    if (int rc = check_launch("rcp_kv8_attn")) return rc;
+    if (!one && plan.chunks == 1) return RCP_OK;
+    const dim3 grid(static_cast<unsigned>(c.H_q), static_cast<unsigned>(one ? c.sequences : c.rows));
+    auto merge = [&](auto kernel) { enqueue(kernel, grid, 512, 0, st, a); };
+    if (one) c.D == 128 ? merge(&kv8_decode_merge_kernel<128>) : merge(&kv8_decode_merge_kernel<64>);
+    else c.D == 128 ? merge(&kv8_prompt_merge_kernel<128>) : merge(&kv8_prompt_merge_kernel<64>);
+    return check_launch("rcp_kv8_attn(merge)");
+}
+
+}  // namespace rcp

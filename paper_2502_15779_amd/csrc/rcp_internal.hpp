@@ -125,6 +125,35 @@ int launch_gemv_sequence(const rcp_gemv_step* steps, int n, void* workspace, hip
 bool gemv_oneshot_applies(int N, int K, bool fused);
 int launch_gemv_oneshot(const void* packed, const void* codebook, int N, int K, const void* x, int x_dt, const void* scale,
                         float clip_ratio, void* out, rcp_dtype out_dt, int32_t* P, void* xq_out, void* scale_out, hipStream_t st);
+// paged 8-bit cache (kv8_append.hip, kv8_attn.hip)
+struct Kv8AppendCall {
+    const void *k, *v, *q;
+    void* q_out;
+    long long k_stride, v_stride, q_stride;
+    rcp_dtype dtype;
+    const float* rope;
+    const int *starts, *lengths, *table;
+    int rows, sequences, width, shift, n_pages, H, H_q, D, rotate;
+    void *k_codes, *v_codes;
+    float *k_scales, *v_scales;
+};
+int launch_kv8_append(const Kv8AppendCall& c, hipStream_t st);
+struct Kv8AttnCall {
+    const void* q;
+    rcp_dtype q_dtype, out_dtype;
+    const int *starts, *lengths, *table;
+    int rows, sequences, width, shift, n_pages, H_q, H_kv, D;
+    const void *k_codes, *v_codes;
+    const float *k_scales, *v_scales;
+    float softmax_scale;
+    void *out, *workspace;
+};
+size_t kv8_workspace_bytes(int rows, int sequences, int H_q, int H_kv, int D, bool one);
+int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st);
+// low-rank adapters beside a shared projection (lowrank.hip)
+size_t lowrank_workspace_bytes(int M, int N, int K, int r);
+int launch_lowrank(const void* x, rcp_dtype dt, int M, int N, int K, int r, int adapters, const void* A, const void* B, const int* which,
+                   const float* scaling, const void* base, void* out, rcp_dtype out_dt, void* workspace, hipStream_t st);
 int gemv_variant(int N, int K, int M);  // 1 vector-ALU kernel, 2 matrix-core kernel: what launch_gemv picks
 
 // ---- small device helpers ------------------------------------------------------------

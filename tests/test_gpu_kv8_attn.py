@@ -1,0 +1,300 @@
+"""Attention over the paged 8-bit cache against 64 bits.
+
+Tolerances, from the formula: a weight w_t is off by a relative e_w = (half step of its binary16 form: 2^-12 of what it is rounded to, at most 2^-11 of it;
+2^-22 as a pair) + 2 x the error of its score.  Scores: D exact products summed in binary32, a few factors, and the exponential: at most
+(D + 16) 2^-24 of softmax_scale sum |q_d K_td| (a binary32 query enters as a pair: 2^-21 more).  The sums over n tokens round n times in binary32.
+So |out - exact| <= (e_w + (n + 16) 2^-24) * 2 sum_t w_t |V_t| (numerator and denominator) + half a step of the result's type."""
+import math
+
+import pytest
+import torch
+
+import kv8_reference as ref
+import paper_2502_15779_amd as rcp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _int(v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def _cache(g, n_pages, H, page, D, junk=True):
+    """Codes and scales of every page; `junk`: all of it NaN codes, for the tests that fill in what a call may see."""
+    out = []
+    for _ in range(2):
+        codes = (torch.randn((n_pages, H, page, D), generator=g) * 60).clamp(-448, 448).to(ref.E4M3)
+        out += [codes, torch.exp2(torch.randint(-8, -4, (n_pages, H), generator=g).float())]
+    return out
+
+
+def _hide(caches, table, lengths):
+    """NaN codes in every slot that no sequence has reached."""
+    n_pages, H, page, D = caches[0].shape
+    live = torch.zeros((n_pages, page), dtype=torch.bool)
+    for b, n in enumerate(lengths):
+        for t in range(min(n, table.shape[1] * page)):
+            p = int(table[b, t // page])
+            if 0 <= p < n_pages:
+                live[p, t % page] = True
+    for i in (0, 2):
+        raw = caches[i].view(torch.uint8)
+        raw[(~live)[:, None, :, None].expand_as(raw)] = 0x7f
+    return caches
+
+
+def _tolerance(exact, mag, size, seen, q, out_dtype, one):
+    D = q.shape[-1]
+    pair = out_dtype == torch.float32 or (one and out_dtype == torch.float16)
+    score = ((D + 16) * 2.0 ** -24 + (2.0 ** -21 if q.dtype == torch.float32 else 0.0)) * size
+    weight = (2.0 ** -22 if pair else 2.0 ** -11) + 2 * score
+    return (weight + (seen + 16) * 2.0 ** -24) * 2 * mag + torch.finfo(out_dtype).eps / 2 * exact.abs() + 1e-30
+
+
+def _check(q, lengths, starts, table, caches, scale, out_dtype, **more):
+    dev = [t.to(DEV) for t in caches]
+    out = torch.full(q.shape, 5.0, dtype=out_dtype, device=DEV)
+    got = rcp.kv8_attn(q.to(DEV), _int(lengths).to(DEV), table.to(DEV), *dev, scale, starts=None if starts is None else _int(starts).to(DEV), out=out, **more)
+    torch.cuda.synchronize()
+    assert got is out
+    exact, mag, size, seen = ref.attention(q, lengths, starts, table, *caches, scale)
+    nobody = exact.isnan()
+    got = got.cpu().double()
+    assert bool((got[nobody] == 5.0).all()), "rows of no sequence were written"
+    off = (got - exact).abs()[~nobody]
+    tol = _tolerance(exact, mag, size, seen, q, out_dtype, starts is None)[~nobody]
+    assert bool(got[~nobody].isfinite().all()) and bool((off <= tol).all()), f"off by {float(off.max()):.2e}, {float((off / tol).max()):.2f} of what is allowed"
+    return out
+
+
+def _table(g, lengths, page, n_pages, extra=0):
+    width = max(-(-n // page) for n in lengths) + extra
+    ids = torch.randperm(n_pages, generator=g)[:width * len(lengths)]
+    return ids.view(len(lengths), width).int()
+
+
+@pytest.mark.parametrize("D,page,H,rep,dtype,out", [
+    (128, 64, 2, 4, "bf16", "bf16"), (128, 16, 3, 1, "f16", "f32"), (128, 128, 1, 16, "f32", "f32"), (128, 32, 2, 17, "f16", "f16"), (128, 32, 1, 40, "bf16", "f32"),
+    (64, 16, 2, 4, "f16", "f16"), (64, 128, 1, 3, "f32", "bf16"), (64, 32, 4, 2, "bf16", "f16"), (64, 64, 1, 1, "f32", "f16"), (128, 64, 1, 8, "f16", "bf16")])
+def test_one_token_each(D, page, H, rep, dtype, out):
+    """Lengths of 0 and 1, around tiles and pages, with NaN codes in every slot beyond them."""
+    print("one token each", D, page, H, rep, dtype, out, flush=True)
+    g = torch.Generator().manual_seed(D + page + rep)
+    lengths = [0, 1, 15, 16, 17, 63, 64, 65, 127, 129, 300]
+    n = sum(-(-x // page) + 1 for x in lengths) * 4
+    table = _table(g, lengths, page, max(n, 11 * (300 // page + 2)), 1)
+    caches = _hide(_cache(g, max(n, 11 * (300 // page + 2)), H, page, D), table, lengths)
+    q = (1.5 * torch.randn((len(lengths), H * rep, D), generator=g)).to(DTYPES[dtype])
+    _check(q, lengths, None, table, caches, D ** -0.5, DTYPES[out])
+
+
+@pytest.mark.parametrize("B,length,H,rep,D", [(1, 5000, 2, 4, 128), (1, 3001, 1, 1, 64), (3, 2500, 1, 2, 128), (70, 130, 1, 2, 64), (1, 64, 1, 1, 128)])
+def test_long_and_many(B, length, H, rep, D):
+    """Sequences in many chunks, more sequences than a wavefront has lanes."""
+    print("long", B, length, H, rep, D, flush=True)
+    g = torch.Generator().manual_seed(B + length)
+    lengths = [max(1, length - 17 * b) for b in range(B)]
+    if B > 60:
+        lengths[65] = 0
+    n = B * (length // 64 + 1)
+    table = _table(g, lengths, 64, n)
+    q = torch.randn((B, H * rep, D), generator=g).half()
+    _check(q, lengths, None, table, _cache(g, n, H, 64, D), D ** -0.5, torch.float32)
+
+
+@pytest.mark.parametrize("D,page,H,rep,dtype,out", [
+    (128, 64, 2, 4, "bf16", "bf16"), (128, 16, 1, 1, "f16", "f16"), (128, 128, 1, 3, "f32", "f32"), (128, 32, 1, 20, "f16", "f32"),
+    (64, 16, 2, 4, "f16", "f16"), (64, 128, 1, 8, "bf16", "f32"), (64, 32, 2, 1, "f32", "bf16"), (64, 64, 1, 2, "f32", "f32")])
+def test_ragged_new_tokens(D, page, H, rep, dtype, out):
+    """Prompts from nothing, chunks behind a context, one token, none, more new tokens than the length; padding rows before and behind."""
+    print("ragged", D, page, H, rep, dtype, out, flush=True)
+    g = torch.Generator().manual_seed(2 * D + page + rep)
+    new = [5, 0, 70, 1, 33, 130, 4]
+    lengths = [5, 80, 70, 200, 161, 131, 2]
+    starts = [1]
+    for x in new:
+        starts.append(starts[-1] + x)
+    n = len(lengths) * (200 // page + 1)
+    table = _table(g, lengths, page, n)
+    caches = _hide(_cache(g, n, H, page, D), table, lengths)
+    q = (1.5 * torch.randn((starts[-1] + 2, H * rep, D), generator=g)).to(DTYPES[dtype])
+    _check(q, lengths, starts, table, caches, D ** -0.5, DTYPES[out])
+
+
+@pytest.mark.parametrize("H,rep,n,length", [(64, 4, 300, 300), (32, 4, 700, 900), (1, 1, 3, 4000)])
+def test_rows_that_fill_the_device_and_a_few_behind_a_long_context(H, rep, n, length):
+    """Enough tiles of rows that no row is split, and a few rows whose context is (checked on some heads)."""
+    D, page = 64, 64
+    g = torch.Generator().manual_seed(n)
+    pages = -(-length // page)
+    table = torch.randperm(pages, generator=g).int()[None]
+    caches = _cache(g, pages, H, page, D)
+    q = torch.randn((n, H * rep, D), generator=g).half()
+    dev = [t.to(DEV) for t in caches]
+    out = rcp.kv8_attn(q.to(DEV), _int([length]).to(DEV), table.to(DEV), *dev, 0.125, starts=_int([0, n]).to(DEV)).cpu().double()
+    for h in {0, H // 2, H - 1}:
+        some = sorted({0, 1, 31, 32, 127, n - 2, n - 1} & set(range(n)))
+        for i in some:   # a row alone is a one-token call of a shorter sequence
+            exact, mag, size, seen = ref.attention(q[i:i + 1, h * rep:h * rep + rep], [length - n + i + 1], None, table, *[t[:, h:h + 1].contiguous() for t in caches], 0.125)
+            tol = _tolerance(exact, mag, size, seen, q, torch.float32, False)
+            assert bool(((out[i:i + 1, h * rep:h * rep + rep] - exact).abs() <= tol).all()), (h, i)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_entries_that_are_no_page(one):
+    """Their tokens are not attended to; a row without any token gets zeros."""
+    D, page, H, rep = 128, 16, 2, 2
+    g = torch.Generator().manual_seed(3)
+    caches = _cache(g, 7, H, page, D)
+    table = _int([[-1, 3, 7, 2, 5], [-1, -1, 2 ** 31 - 1, -2 ** 31, 6], [0, 1, -1, -1, 4], [-1, -1, -1, -1, -1]])
+    if one:
+        cases, starts, rows = [[80, 64, 48, 80], [17, 65, 33, 1], [10, 80, 1000, 0], [-3, 81, 79, 16]], None, 4
+    else:
+        cases, starts, rows = [[80, 80, 48, 80], [40, 66, 90, 20]], [0, 40, 60, 81, 100], 100
+    for lengths in cases:
+        q = torch.randn((rows, H * rep, D), generator=g).half()
+        clipped = [min(n, 80) if one else n for n in lengths]
+        for out in (torch.float16, torch.float32):
+            if one:
+                got = rcp.kv8_attn(q.to(DEV), _int(lengths).to(DEV), table.to(DEV), *[t.to(DEV) for t in caches], 0.09, out_dtype=out).cpu().double()
+                exact, mag, size, seen = ref.attention(q, clipped, None, table, *caches, 0.09)
+                assert bool(((got - exact).abs() <= _tolerance(exact, mag, size, seen, q, out, True)).all())
+                assert bool((got[3] == 0).all())
+            else:
+                _check(q, lengths, starts, table, caches, 0.09, out)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_pages_of_very_different_scales(one):
+    """A page of large values and little attention must not push the others out of the weights' 16 bits, nor a page of tiny ones be lost; a zeroed
+    page (scale 0) stands for zeros."""
+    D, page, H = 128, 16, 1
+    g = torch.Generator().manual_seed(4)
+    caches = _cache(g, 6, H, page, D)
+    caches[3][:, 0] = torch.tensor([2.0 ** 60, 1.0, 2.0 ** -38, 2.0 ** 100, 0.0, 2.0 ** -6])
+    caches[1][:, 0] = 2.0 ** -6
+    # the pages of large values get scores far below the others: their keys oppose the query
+    q = torch.randn((3, 2, D), generator=g).half()
+    away = -torch.sign(q[0, 0].float())
+    for p, strength in ((0, 448.0), (3, 448.0)):
+        caches[0][p, 0] = (away * strength).expand(page, D).to(ref.E4M3)
+    q[:] = q[0, 0].abs() * torch.sign(q[0, 0])
+    lengths, starts, table = ([96, 90, 41], None, _int([[0, 1, 2, 3, 4, 5], [5, 4, 3, 2, 1, 0], [2, 2, 2, 2, 2, 2]])) if one else \
+        ([96], [0, 3], _int([[0, 1, 2, 3, 4, 5]]))
+    for scale in (0.1, 0.05):
+        for out in (torch.float32, torch.bfloat16):
+            _check(q, lengths, starts, table, caches, scale, out)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_rows_are_independent(one):
+    """An infinite or NaN query, or one of another magnitude, changes no other row or head."""
+    D, page, H, rep = 64, 32, 2, 4
+    g = torch.Generator().manual_seed(5)
+    caches = [t.to(DEV) for t in _cache(g, 8, H, page, D)]
+    table = torch.arange(8).int().view(2, 4).to(DEV)
+    rows, lengths = (2, [100, 77]) if one else (50, [100, 90])
+    starts = None if one else _int([0, 30, 50]).to(DEV)
+    q = torch.randn((rows, H * rep, D), generator=g).bfloat16().to(DEV)
+    run = lambda x: rcp.kv8_attn(x, _int(lengths).to(DEV), table, *caches, 0.125, starts=starts)
+    plain = run(q)
+    for bad in (float("inf"), float("nan"), 1e30, 0.0):
+        x = q.clone()
+        x[1, 3] = bad
+        got = run(x)
+        keep = torch.ones((rows, H * rep), dtype=torch.bool, device=DEV)
+        keep[1, 3] = False
+        assert torch.equal(got[keep], plain[keep]), bad
+        if bad == 0.0:
+            assert bool(got[1, 3].isfinite().all())
+
+
+def test_a_token_behind_a_row_never_enters():
+    """Changing the tokens after a row's own leaves its result as it was, to the last bit."""
+    D, page, H = 128, 16, 1
+    g = torch.Generator().manual_seed(6)
+    caches = _cache(g, 8, H, page, D)
+    q = torch.randn((60, 2, D), generator=g).half().to(DEV)
+    table, starts = torch.arange(8).int()[None].to(DEV), _int([0, 60]).to(DEV)
+    run = lambda c: rcp.kv8_attn(q, _int([100]).to(DEV), table, *[t.to(DEV) for t in c], 0.09, starts=starts)
+    a = run(caches)
+    other = [t.clone() for t in caches]
+    for i in (0, 2):
+        other[i].view(torch.uint8)[5, :, 8:] = 0x7e   # positions 88 ..: the largest code, in the page of rows 40 to 55
+        other[i].view(torch.uint8)[6] = 0xfe
+    b = run(other)
+    assert torch.equal(a[:48], b[:48]) and not torch.equal(a[48:], b[48:])
+
+
+def test_outputs_made_here_and_workspaces_given():
+    D, H = 64, 2
+    g = torch.Generator().manual_seed(7)
+    caches = [t.to(DEV) for t in _cache(g, 4, H, 16, D)]
+    table, q = torch.arange(4).int().view(2, 2).to(DEV), torch.randn((9, 4, D), generator=g).half().to(DEV)
+    starts = _int([2, 5, 7]).to(DEV)
+    out = rcp.kv8_attn(q, _int([20, 9]).to(DEV), table, *caches, 0.1, starts=starts, out_dtype=torch.bfloat16)
+    assert out.dtype == torch.bfloat16 and bool((out[:2] == 0).all()) and bool((out[7:] == 0).all()) and bool((out[2:7] != 0).any())
+    work = torch.empty(rcp.kv8_workspace_bytes(9, 2, 4, H, D, False), dtype=torch.uint8, device=DEV)
+    again = rcp.kv8_attn(q, _int([20, 9]).to(DEV), table, *caches, 0.1, starts=starts, out_dtype=torch.bfloat16, workspace=work)
+    assert torch.equal(out, again)
+    assert rcp.kv8_attn(q[:0], _int([20, 9]).to(DEV), table, *caches, 0.1, starts=starts).shape == (0, 4, D)
+    with pytest.raises(rcp.RcpError) as e:
+        rcp.kv8_attn(q, _int([20, 9]).to(DEV), table, *caches, 0.1, starts=starts, workspace=work[:16])
+    assert e.value.code == -5
+    for bad in (dict(starts=_int([2, 5]).to(DEV)), dict(starts=starts.long()), dict(starts=_int([2, 5, 7])), dict(starts=None), dict(out=out[:3], starts=starts)):
+        with pytest.raises(ValueError):
+            rcp.kv8_attn(q, _int([20, 9]).to(DEV), table, *caches, 0.1, **bad)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_a_capture_follows_lengths_and_tables(one):
+    """Replayed on other lengths, starts, tables and queries, against eager calls between the replays; its chunks are cut anew each time."""
+    D, page, H, rep, B = 128, 16, 2, 4, 3
+    g = torch.Generator().manual_seed(8)
+    caches = [t.to(DEV) for t in _cache(g, 120, H, page, D)]
+    rows = B if one else 40
+    q, out = torch.zeros((rows, H * rep, D), dtype=torch.float16, device=DEV), torch.zeros((rows, H * rep, D), device=DEV)
+    lengths, table = _int([1] * B).to(DEV), torch.zeros((B, 40), dtype=torch.int32, device=DEV)
+    starts = None if one else _int([0, 10, 20, 30]).to(DEV)
+    work = torch.empty(rcp.kv8_workspace_bytes(rows, B, H * rep, H, D, one), dtype=torch.uint8, device=DEV)
+    call = lambda o, w: rcp.kv8_attn(q, lengths, table, *caches, 0.09, starts=starts, out=o, workspace=w)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(out, work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(out, work)
+    for n, s in (([600, 1, 70], [0, 40, 40, 40]), ([0, 640, 333], [0, 0, 25, 39]), ([64, 64, 64], [3, 20, 21, 40]), ([5, 6, 7], [0, 5, 11, 18])):
+        lengths.copy_(_int(n))
+        if not one:
+            starts.copy_(_int(s))
+        table.copy_(torch.randperm(120, generator=g).view(B, 40))
+        q.copy_(torch.randn(q.shape, generator=g))
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = torch.full_like(out, 9.0)
+        call(want, torch.empty_like(work))
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and not bool((want[:1] == 9.0).all() and one)
+
+
+def test_on_the_current_stream():
+    """On a side stream that first keeps the GPU busy and then writes the inputs: any other stream would read the old ones."""
+    D, H = 64, 2
+    g = torch.Generator().manual_seed(9)
+    caches = [t.to(DEV) for t in _cache(g, 4, H, 16, D)]
+    table, lengths, new = torch.arange(4).int().view(2, 2).to(DEV), _int([20, 9]).to(DEV), torch.randn((2, 4, D), generator=g).half().to(DEV)
+    want = rcp.kv8_attn(new, lengths, table, *caches, 0.1)
+    q, out = torch.zeros_like(new), torch.zeros_like(want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        q.copy_(new)
+        rcp.kv8_attn(q, lengths, table, *caches, 0.1, out=out)
+    side.synchronize()
+    assert torch.equal(out, want) and math.isfinite(float(out.sum()))
