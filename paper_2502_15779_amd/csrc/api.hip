@@ -858,8 +858,8 @@ int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const v
 static int check_lowrank(const char* fn, int M, int N, int K, int r)
 {
     if (M < 0 || M > RCP_LOWRANK_MAX_M) return fail(RCP_ERR_SHAPE, "%s: M=%d outside 0..%d", fn, M, RCP_LOWRANK_MAX_M);
-    if (N < 1 || N % 4 != 0 || N > (1 << 24)) return fail(RCP_ERR_SHAPE, "%s: N=%d must be a positive multiple of 4", fn, N);
-    if (K < 1 || K % 32 != 0 || K > (1 << 24)) return fail(RCP_ERR_SHAPE, "%s: K=%d must be a positive multiple of 32", fn, K);
+    if (N < 1 || N % 4 != 0 || N > (1 << 24)) return fail(RCP_ERR_SHAPE, "%s: N=%d must be a positive multiple of 4, at most 2^24", fn, N);
+    if (K < 1 || K % 32 != 0 || K > (1 << 20)) return fail(RCP_ERR_SHAPE, "%s: K=%d must be a positive multiple of 32, at most 2^20", fn, K);
     if (r < 1 || r % 8 != 0 || r > RCP_LOWRANK_MAX_R)
         return fail(RCP_ERR_SHAPE, "%s: r=%d must be a positive multiple of 8, at most %d", fn, r, RCP_LOWRANK_MAX_R);
     return RCP_OK;

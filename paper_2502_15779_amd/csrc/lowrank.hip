@@ -37,8 +37,7 @@ struct LowrankArgs {
     const float* scaling;
     void* out;
     float* part;  // [splits][M][r]
-    int M, N, K, r, adapters, splits, chunk;  // chunk: columns of a split, a multiple of 4 * LOWRANK_STEP
-    int slots, columns;                       // first kernel: leaders side by side; second: outputs of a workgroup, a multiple of 128
+    int M, N, K, r, adapters, splits, chunk, slots;  // chunk: columns of a split; slots: leaders side by side in the first kernel
 };
 
 // the adapter of token m, -1 for none
@@ -48,82 +47,170 @@ __device__ __forceinline__ int lowrank_adapter(const LowrankArgs& a, int m)
     return static_cast<unsigned>(id) < static_cast<unsigned>(a.adapters) ? id : -1;
 }
 
-// the lanes among `tokens` whose adapter no lower lane has
-__device__ __forceinline__ unsigned long long lowrank_leaders(int id, int tokens)
+// The lanes among the first `tokens` whose adapter no lower lane has; `order`: how many of those come before the one of a lane's own adapter.
+__device__ __forceinline__ unsigned long long lowrank_leaders(int id, int tokens, int& order)
 {
     unsigned long long rest = __builtin_amdgcn_ballot_w64(id >= 0), leaders = 0;
     if (tokens < 64) rest &= (1ull << tokens) - 1;
-    while (rest != 0) {  // at most one round for each lane
+    order = 0;
+    for (int n = 0; rest != 0; ++n) {  // at most one round for each lane
         const int at = __builtin_ctzll(rest);
+        const bool same = id == __builtin_amdgcn_readlane(id, at);
         leaders |= 1ull << at;
-        rest &= ~__builtin_amdgcn_ballot_w64(id == __builtin_amdgcn_readlane(id, at));
+        rest &= ~__builtin_amdgcn_ballot_w64(same);
+        order = same ? n : order;
     }
     return leaders;
 }
 
-// Workgroup = (split of K, slot of leaders, TT x 16 tokens); each wavefront sums a quarter of the split.
-template <int DT, int TT, int NR>
-__global__ __launch_bounds__(256) void lowrank_in_kernel(LowrankArgs a)
+// Few tokens: workgroup = (split of K, slot of leaders, sixteen tokens); each wavefront sums a quarter of the split, from registers, two blocks of
+// two steps ahead of the products (rows = ranks, columns = tokens).
+template <int DT, int NR>
+__global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
 {
-    __shared__ float red[3][TT][NR][256];
+    constexpr int U = 2, BLOCK = LOWRANK_STEP * U;
+    __shared__ float red[3][NR][256];
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = static_cast<int>(blockIdx.z) * 16 * TT;
-    const int id = lane < 16 * TT ? lowrank_adapter(a, m0 + lane) : -1;
-    unsigned long long leaders = lowrank_leaders(id, 16 * TT);
+    const int m0 = static_cast<int>(blockIdx.z) * 16;
+    const int id = lane < 16 ? lowrank_adapter(a, m0 + lane) : -1;
+    int order;
+    unsigned long long leaders = lowrank_leaders(id, 16, order);
     const int quarter = a.chunk / 4, k0 = static_cast<int>(blockIdx.x) * a.chunk + quarter * wave, k1 = min(a.K, k0 + quarter);
-    const auto* const x = static_cast<const One<DT>*>(a.x);
+    const auto* const x = static_cast<const One<DT>*>(a.x) + static_cast<size_t>(min(m0 + i, a.M - 1)) * a.K + 8 * g;  // beyond the last token: that again
     for (int slot = 0; leaders != 0; ++slot, leaders &= leaders - 1) {
         if (slot % a.slots != static_cast<int>(blockIdx.y)) continue;  // uniform
         const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
-        const auto* const A = static_cast<const One<DT>*>(a.A) + static_cast<size_t>(adapter) * a.r * a.K;
+        const auto* const A = static_cast<const One<DT>*>(a.A) + static_cast<size_t>(adapter) * a.r * a.K + 8 * g;
         for (int r0 = 0; r0 < a.r; r0 += 16 * NR) {
-            v4f acc[TT][NR];
+            v4f acc[NR];
+            const One<DT>* rows[NR];
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
+            for (int n = 0; n < NR; ++n) {
+                acc[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                rows[n] = A + static_cast<size_t>(min(r0 + 16 * n + i, a.r - 1)) * a.K;
+            }
+            Eight<DT> xv[2][U], av[2][U][NR];
+            auto load = [&](int buf, int k) {  // columns beyond the end: the last ones again, which no product takes
 #pragma unroll
-                for (int n = 0; n < NR; ++n) acc[t][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            size_t xat[TT], aat[NR];  // rows beyond the last token or rank repeat it
+                for (int u = 0; u < U; ++u) {
+                    const int at = min(k + LOWRANK_STEP * u, k1 - LOWRANK_STEP);
+                    xv[buf][u] = *reinterpret_cast<const Eight<DT>*>(x + at);
 #pragma unroll
-            for (int t = 0; t < TT; ++t) xat[t] = static_cast<size_t>(min(m0 + 16 * t + i, a.M - 1)) * a.K + 8 * g;
+                    for (int n = 0; n < NR; ++n) av[buf][u][n] = *reinterpret_cast<const Eight<DT>*>(rows[n] + at);
+                }
+            };
+            auto take = [&](int buf, int k) {
 #pragma unroll
-            for (int n = 0; n < NR; ++n) aat[n] = static_cast<size_t>(min(r0 + 16 * n + i, a.r - 1)) * a.K + 8 * g;
-#pragma unroll 4
-            for (int k = k0; k < k1; k += LOWRANK_STEP) {
-                Eight<DT> xv[TT], av[NR];
+                for (int u = 0; u < U; ++u)
+                    if (k + LOWRANK_STEP * u < k1) {  // uniform
 #pragma unroll
-                for (int t = 0; t < TT; ++t) xv[t] = *reinterpret_cast<const Eight<DT>*>(x + xat[t] + k);
-#pragma unroll
-                for (int n = 0; n < NR; ++n) av[n] = *reinterpret_cast<const Eight<DT>*>(A + aat[n] + k);
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) acc[t][n] = lowrank_mfma<DT>(xv[t], av[n], acc[t][n]);
+                        for (int n = 0; n < NR; ++n) acc[n] = lowrank_mfma<DT>(av[buf][u][n], xv[buf][u], acc[n]);
+                    }
+            };
+            if (k0 < k1) {
+                load(0, k0);
+                load(1, k0 + BLOCK);
+                for (int k = k0; k < k1; k += 2 * BLOCK) {
+                    take(0, k);
+                    if (k + 2 * BLOCK < k1) load(0, k + 2 * BLOCK);
+                    take(1, k + BLOCK);
+                    if (k + 3 * BLOCK < k1) load(1, k + 3 * BLOCK);
+                }
             }
             if (wave > 0) {
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) *reinterpret_cast<v4f*>(&red[wave - 1][t][n][4 * lane]) = acc[t][n];
+                for (int n = 0; n < NR; ++n) *reinterpret_cast<v4f*>(&red[wave - 1][n][4 * lane]) = acc[n];
             }
             __syncthreads();
-            if (wave == 0) {
+            if (wave == 0 && __shfl(id, i, 64) == adapter) {
+                float* const to = a.part + (static_cast<size_t>(blockIdx.x) * a.M + m0 + i) * a.r;
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
+                for (int n = 0; n < NR; ++n) {
+                    const int rank = r0 + 16 * n + 4 * g;
 #pragma unroll
-                    for (int n = 0; n < NR; ++n) {
-                        v4f s = acc[t][n];
-#pragma unroll
-                        for (int w = 0; w < 3; ++w) s += *reinterpret_cast<const v4f*>(&red[w][t][n][4 * lane]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int at = 16 * t + 4 * g + j, rank = r0 + 16 * n + i;
-                            if (__shfl(id, at, 64) == adapter && rank < a.r)
-                                a.part[(static_cast<size_t>(blockIdx.x) * a.M + m0 + at) * a.r + rank] = s[j];
-                        }
-                    }
+                    for (int w = 0; w < 3; ++w) acc[n] += *reinterpret_cast<const v4f*>(&red[w][n][4 * lane]);
+                    if (rank < a.r) *reinterpret_cast<v4f*>(to + rank) = acc[n];
+                }
             }
             __syncthreads();
+        }
+    }
+}
+
+// Many tokens: workgroup = (split of K, slot of leaders, 64 tokens), sixteen tokens of each wavefront.  x and A come through LDS in stages of 128 columns, two
+// of them, so that a load takes 256 bytes of a row: read in the products' own order, 64 bytes of each of sixteen rows whose distance is a multiple of
+// 4 KB meet in one channel of the cache (2001 tokens, K = 14336: 27 us).  Piece p (16 bytes) of row n stands at place p ^ (n % 16).
+constexpr int LOWRANK_STAGE = 128;
+
+__device__ __forceinline__ void lowrank_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* to, int offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+}
+
+template <int DT, int NR>
+__global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
+{
+    constexpr int ROW = LOWRANK_STAGE * 2;  // bytes
+    __shared__ __attribute__((aligned(16))) unsigned char xs[2][64 * ROW], as[2][16 * NR * ROW];
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int m0 = static_cast<int>(blockIdx.z) * 64;
+    const int id = lowrank_adapter(a, m0 + lane);
+    int order;
+    unsigned long long leaders = lowrank_leaders(id, 64, order);
+    const int k0 = static_cast<int>(blockIdx.x) * a.chunk, k1 = min(a.K, k0 + a.chunk);
+    const int mine = __shfl(id, 16 * wave + i, 64);
+    const auto resource = [](const void* p, size_t at, size_t rows, size_t K) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + at * K * 2, 0, static_cast<int>(rows * K * 2), 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t xr = resource(a.x, m0, min(64, a.M - m0), a.K);
+    for (int slot = 0; leaders != 0; ++slot, leaders &= leaders - 1) {
+        if (slot % a.slots != static_cast<int>(blockIdx.y)) continue;  // uniform
+        const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
+        for (int r0 = 0; r0 < a.r; r0 += 16 * NR) {
+            const int ranks = min(16 * NR, a.r - r0);
+            const __amdgpu_buffer_rsrc_t ar = resource(a.A, static_cast<size_t>(adapter) * a.r + r0, ranks, a.K);  // ranks beyond the last read zeros
+            auto stage = [&](int k, int buf) {  // four rows a load
+                const int piece = lane & 15;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int row = 16 * wave + 4 * y + (lane >> 4);
+                    lowrank_to_lds(xr, &xs[buf][(16 * wave + 4 * y) * ROW], (row * a.K + k) * 2 + 16 * (piece ^ (row & 15)));
+                }
+#pragma unroll
+                for (int y = 0; y < NR; ++y) {
+                    const int row = 4 * NR * wave + 4 * y + (lane >> 4);
+                    lowrank_to_lds(ar, &as[buf][(4 * NR * wave + 4 * y) * ROW], (row * a.K + k) * 2 + 16 * (piece ^ (row & 15)));
+                }
+            };
+            v4f acc[NR];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) acc[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            stage(k0, 0);
+            for (int k = k0, buf = 0; k < k1; k += LOWRANK_STAGE, buf ^= 1) {
+                __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the stage is in LDS,
+                __syncthreads();                // everybody's is, and the other buffer has been read
+                if (k + LOWRANK_STAGE < k1) stage(k + LOWRANK_STAGE, buf ^ 1);
+#pragma unroll
+                for (int s = 0; s < LOWRANK_STAGE / LOWRANK_STEP; ++s) {
+                    if (k + LOWRANK_STEP * s >= k1) break;  // uniform
+                    const int at = ((4 * s + g) ^ i) * 16;
+                    const Eight<DT> xv = *reinterpret_cast<const Eight<DT>*>(&xs[buf][(16 * wave + i) * ROW + at]);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+                        acc[n] = lowrank_mfma<DT>(*reinterpret_cast<const Eight<DT>*>(&as[buf][(16 * n + i) * ROW + at]), xv, acc[n]);
+                }
+            }
+            if (mine == adapter) {
+                float* const to = a.part + (static_cast<size_t>(blockIdx.x) * a.M + m0 + 16 * wave + i) * a.r;
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    const int rank = r0 + 16 * n + 4 * g;
+                    if (rank < a.r) *reinterpret_cast<v4f*>(to + rank) = acc[n];
+                }
+            }
+            __syncthreads();  // the next round fills the buffers anew
         }
     }
 }
@@ -140,22 +227,9 @@ __device__ __forceinline__ Eight<DT> lowrank_round(float (&v)[8])  // and leaves
     return h;
 }
 
+// four results of a row from index i on
 template <int DT>
-__device__ __forceinline__ void lowrank_load4(const void* p, size_t i, float (&v)[4])
-{
-    if constexpr (DT == RCP_F32) {
-        const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-    } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-        const uint16_t h[4] = {static_cast<uint16_t>(w.x), static_cast<uint16_t>(w.x >> 16), static_cast<uint16_t>(w.y), static_cast<uint16_t>(w.y >> 16)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = DT == RCP_F16 ? half_bits_to_float(h[e]) : bf16_bits_to_float(h[e]);
-    }
-}
-
-template <int DT>
-__device__ __forceinline__ void lowrank_store4(void* p, size_t i, const float (&v)[4])
+__device__ __forceinline__ void lowrank_store4(void* p, size_t i, const float* v)
 {
     if constexpr (DT == RCP_F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
     else {
@@ -169,151 +243,318 @@ __device__ __forceinline__ void lowrank_store4(void* p, size_t i, const float (&
     }
 }
 
-// Workgroup = (`columns` outputs, sixteen tokens).  Products with rows = outputs and columns = tokens: a lane holds token lane % 16 and, of
-// 32 outputs in two products, eight neighbouring ones (row 4 g + j of product p is output 8 g + 4 p + j).
-template <int DT, int OUT>
-__global__ __launch_bounds__(256) void lowrank_out_kernel(LowrankArgs a)
+template <int DT>
+using Raw4 = std::conditional_t<DT == RCP_F32, float4, uint2>;
+
+template <int DT>
+__device__ __forceinline__ Raw4<DT> lowrank_load4(const void* p, size_t i)
 {
-    constexpr int PIECES = DT == RCP_F16 ? 2 : 3;
-    extern __shared__ float sums[];  // t of the tile: [16][stride]
-    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = static_cast<int>(blockIdx.y) * 16, padded = (a.r + 31) / 32 * 32, stride = padded + 4;
-    const int id = lane < 16 ? lowrank_adapter(a, m0 + lane) : -1;
-    const unsigned long long leaders = lowrank_leaders(id, 16);
-    const int mine = __shfl(id, i, 64);
-    for (int at = tid; at < 16 * padded; at += 256) {
-        const int m = at / padded, rank = at - m * padded, adapter = lowrank_adapter(a, m0 + m);
-        float s = 0.0f;
-        if (adapter >= 0 && rank < a.r) {
-            for (int k = 0; k < a.splits; ++k) s += a.part[(static_cast<size_t>(k) * a.M + m0 + m) * a.r + rank];
-            s *= a.scaling[adapter];
-        }
-        sums[m * stride + rank] = s;
+    return *reinterpret_cast<const Raw4<DT>*>(static_cast<const char*>(p) + i * (DT == RCP_F32 ? 4 : 2));
+}
+
+template <int DT>
+__device__ __forceinline__ void lowrank_add4(const Raw4<DT>& x, float* v)
+{
+    if constexpr (DT == RCP_F32) {
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    } else {
+        const uint16_t h[4] = {static_cast<uint16_t>(x.x), static_cast<uint16_t>(x.x >> 16), static_cast<uint16_t>(x.y), static_cast<uint16_t>(x.y >> 16)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += DT == RCP_F16 ? half_bits_to_float(h[e]) : bf16_bits_to_float(h[e]);
     }
-    __syncthreads();
-    int E = 14;  // binary16: the token's largest value becomes 2^13 .. 2^14
+}
+
+// scaling t of a tile of sixteen tokens, summed over the splits, into LDS [16][PADDED + 4] (zeros for ranks beyond the last and tokens without an adapter)
+template <int PADDED>
+__device__ __forceinline__ void lowrank_total(const LowrankArgs& a, int m0, int id, float* sums)
+{
+    constexpr int MINE = 16 * PADDED / 256;  // values of a thread
+    float t[MINE], scale[MINE];
+    const float* from[MINE];
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) {  // what no token has is read, too (it lies in the workspace), and dropped: no branches between the loads
+        const int at = threadIdx.x + 256 * x, token = at / PADDED, rank = at % PADDED;
+        scale[x] = a.scaling[max(__shfl(id, token, 64), 0)];
+        from[x] = a.part + static_cast<size_t>(min(m0 + token, a.M - 1)) * a.r + min(rank, a.r - 1);
+        t[x] = 0.0f;
+    }
+    const size_t next = static_cast<size_t>(a.M) * a.r;
+    int k = 0;
+    for (; k + 4 <= a.splits; k += 4)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) t[x] += from[x][(k + y) * next];
+    for (; k < a.splits; ++k)
+#pragma unroll
+        for (int x = 0; x < MINE; ++x) t[x] += from[x][k * next];
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) {
+        const int at = threadIdx.x + 256 * x, token = at / PADDED, rank = at % PADDED;
+        sums[token * (PADDED + 4) + rank] = __shfl(id, token, 64) >= 0 && rank < a.r ? t[x] * scale[x] : 0.0f;
+    }
+}
+
+// the t of token lane % 16 as operands; returns E of the binary16 scale: its largest value becomes 2^13 .. 2^14
+template <int DT, int STEPS, int PIECES>
+__device__ __forceinline__ int lowrank_pieces(const float* sums, Eight<DT> (&piece)[STEPS][PIECES])
+{
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    float t[STEPS][8], top = 0.0f;
+    int E = 14;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            t[s][e] = sums[i * (32 * STEPS + 4) + 32 * s + 8 * g + e];
+            top = fmaxf(top, fabsf(t[s][e]));
+        }
     if constexpr (DT == RCP_F16) {
-        float top = 0.0f;
-        for (int rank = 0; rank < padded; ++rank) top = fmaxf(top, fabsf(sums[i * stride + rank]));
+        auto swap = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
+        swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
         E = __builtin_amdgcn_frexp_expf(top);
     }
-    const int end = min(a.N, (static_cast<int>(blockIdx.x) + 1) * a.columns), steps = padded / 32;
-    const auto* const B = static_cast<const One<DT>*>(a.B);
-    for (int n0 = static_cast<int>(blockIdx.x) * a.columns + 32 * wave; n0 < end; n0 += 128) {
-        v4f total[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
-        size_t row[2];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) row[p] = static_cast<size_t>(min(n0 + 8 * (i >> 2) + 4 * p + (i & 3), a.N - 1)) * a.r;
-        for (unsigned long long rest = leaders; rest != 0; rest &= rest - 1) {
-            const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(rest));
-            const auto* const Ba = B + static_cast<size_t>(adapter) * a.N * a.r;
-            v4f acc[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
-            for (int s = 0; s < steps; ++s) {
-                const int rank = 32 * s + 8 * g;
-                Eight<DT> b[2];
+    for (int s = 0; s < STEPS; ++s) {
+        if constexpr (DT == RCP_F16)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[s][e] = ldexpf(t[s][e], 14 - E);
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) piece[s][q] = lowrank_round<DT>(t[s]);
+    }
+    return E;
+}
+
+// rows of B (ranks 32 s + 8 g ..) times t; ranks beyond the last are zeros on both sides
+template <int DT, int STEPS, int PIECES>
+__device__ __forceinline__ v4f lowrank_product(int r, int g, Eight<DT> (&b)[STEPS], const Eight<DT> (&piece)[STEPS][PIECES])
+{
+    v4f acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        if (32 * s >= r) break;  // uniform
+        if (32 * s + 8 * g >= r) b[s] = Eight<DT>{};
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) acc = lowrank_mfma<DT>(b[s], piece[s][q], acc);
+    }
+    return acc;
+}
+
+// Few tokens, so that many have an adapter of their own: workgroup = (32 outputs, sixteen tokens); wavefront w takes the adapters w, w + 4, ... of the tile and
+// writes the rows of their tokens.  Products with rows = outputs, columns = tokens: a lane holds token lane % 16 and four neighbouring outputs.
+template <int DT, int OUT, int STEPS>
+__global__ __launch_bounds__(256) void lowrank_few_out_kernel(LowrankArgs a)
+{
+    constexpr int PIECES = DT == RCP_F16 ? 2 : 3, TOGETHER = 4 / STEPS;  // adapters whose rows of B are under way at a time
+    __shared__ float sums[16 * (32 * STEPS + 4)];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const int m0 = static_cast<int>(blockIdx.y) * 16, n0 = static_cast<int>(blockIdx.x) * 32;
+    const int id = lane < 16 ? lowrank_adapter(a, m0 + lane) : -1;
+    int order;
+    unsigned long long leaders = lowrank_leaders(id, 16, order);
+    const int mine = __shfl(id, i, 64), at = __shfl(order, i, 64);
+    for (int w = 0; w < wave; ++w) leaders &= leaders - 1;  // this wavefront's first one
+    const bool writes = m0 + i < a.M && wave == ((mine >= 0 ? at : i) & 3);
+    const auto* const B = static_cast<const One<DT>*>(a.B);
+    Eight<DT> b[TOGETHER][2][STEPS];
+    int adapter[TOGETHER];
+    auto load = [&](unsigned long long from) {
+#pragma unroll
+        for (int u = 0; u < TOGETHER; ++u) {
+            adapter[u] = from != 0 ? __builtin_amdgcn_readlane(id, __builtin_ctzll(from)) : -1;
+            if (adapter[u] >= 0) {  // uniform
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
-                    if (rank < a.r) b[p] = *reinterpret_cast<const Eight<DT>*>(Ba + row[p] + rank);
-                    else
+                    const auto* const row = B + (static_cast<size_t>(adapter[u]) * a.N + min(n0 + 16 * p + i, a.N - 1)) * a.r;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) b[p][e] = static_cast<One<DT>>(0.0f);
-                }
-                float t[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    t[e] = sums[i * stride + rank + e];
-                    if constexpr (DT == RCP_F16) t[e] = ldexpf(t[e], 14 - E);
-                }
-#pragma unroll
-                for (int q = 0; q < PIECES; ++q) {
-                    const Eight<DT> piece = lowrank_round<DT>(t);
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) acc[p] = lowrank_mfma<DT>(b[p], piece, acc[p]);
+                    for (int s = 0; s < STEPS; ++s) b[u][p][s] = *reinterpret_cast<const Eight<DT>*>(row + min(32 * s + 8 * g, a.r - 8));
                 }
             }
-            // only the tokens of this adapter take its products: an infinity in one request's adapter stays with that request
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) total[p][j] = mine == adapter ? acc[p][j] : total[p][j];
+            for (int w = 0; w < 4; ++w) from &= from - 1;
         }
-        const int m = m0 + i;
+        return from;
+    };
+    leaders = load(leaders);
+    Raw4<OUT> base[2];
+    const size_t to = static_cast<size_t>(m0 + i) * a.N + n0 + 4 * g;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const int n = n0 + 8 * g + 4 * p;
-            if (m < a.M && n < end) {
-                float v[4];
-                lowrank_load4<OUT>(a.base, static_cast<size_t>(m) * a.N + n, v);
-                if (mine >= 0) {
+    for (int p = 0; p < 2; ++p)
+        if (writes && n0 + 16 * p + 4 * g < a.N) base[p] = lowrank_load4<OUT>(a.base, to + 16 * p);
+    lowrank_total<32 * STEPS>(a, m0, id, sums);
+    __syncthreads();
+    Eight<DT> piece[STEPS][PIECES];
+    const int E = lowrank_pieces<DT, STEPS, PIECES>(sums, piece);
+    v4f total[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
+    for (;;) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] += DT == RCP_F16 ? ldexpf(total[p][j], E - 14) : total[p][j];
-                }
-                lowrank_store4<OUT>(a.out, static_cast<size_t>(m) * a.N + n, v);
+        for (int u = 0; u < TOGETHER; ++u) {
+            if (adapter[u] < 0) break;  // uniform
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const v4f x = lowrank_product<DT, STEPS, PIECES>(a.r, g, b[u][p], piece);
+                // only the tokens of this adapter take its products: an infinity in one request's adapter stays with that request
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total[p][j] = mine == adapter[u] ? x[j] : total[p][j];
             }
         }
+        if (leaders == 0) break;  // uniform
+        leaders = load(leaders);
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+        if (writes && n0 + 16 * p + 4 * g < a.N) {
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = DT == RCP_F16 ? ldexpf(total[p][j], E - 14) : total[p][j];
+            lowrank_add4<OUT>(base[p], v);
+            lowrank_store4<OUT>(a.out, to + 16 * p, v);
+        }
+}
+
+// Many tokens: workgroup = (512 outputs, sixteen tokens), 128 outputs of each wavefront.  The products pass through LDS, so that base and out are read and
+// written in kilobytes of a row: in the products' own order (32 bytes of each of sixteen rows) 2001 tokens of 4096 outputs took 30 us.
+constexpr int LOWRANK_COLUMNS = 512;
+
+template <int DT, int OUT, int STEPS>
+__global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
+{
+    constexpr int PIECES = DT == RCP_F16 ? 2 : 3, ROW = LOWRANK_COLUMNS + 4;
+    __shared__ __attribute__((aligned(16))) float block[16 * ROW];  // the products; before them, t
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const int m0 = static_cast<int>(blockIdx.x) * 16, n0 = static_cast<int>(blockIdx.y) * LOWRANK_COLUMNS;
+    if (m0 >= a.M) return;  // the grid's width is a multiple of eight
+    const int id = lane < 16 ? lowrank_adapter(a, m0 + lane) : -1;
+    int order;
+    unsigned long long leaders = lowrank_leaders(id, 16, order);
+    const int mine = __shfl(id, i, 64);
+    // rows wave, wave + 4, ... of the tile, eight outputs a lane
+    Raw4<OUT> base[4][2];
+    const int n = n0 + 8 * lane;
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            if (m0 + 4 * y + wave < a.M && n + 4 * p < a.N) base[y][p] = lowrank_load4<OUT>(a.base, static_cast<size_t>(m0 + 4 * y + wave) * a.N + n + 4 * p);
+    Eight<DT> piece[STEPS][PIECES];
+    int E = 14;
+    if (leaders != 0) {  // uniform over the workgroup
+        lowrank_total<32 * STEPS>(a, m0, id, block);
+        __syncthreads();
+        E = lowrank_pieces<DT, STEPS, PIECES>(block, piece);
+        __syncthreads();
+    }
+    for (; leaders != 0; leaders &= leaders - 1) {
+        const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
+        const auto* const B = static_cast<const One<DT>*>(a.B) + static_cast<size_t>(adapter) * a.N * a.r;
+        constexpr int AT_ONCE = 8 / STEPS;  // products whose rows of B are under way at a time
+#pragma unroll
+        for (int c0 = 0; c0 < 8; c0 += AT_ONCE) {
+            Eight<DT> b[AT_ONCE][STEPS];
+#pragma unroll
+            for (int c = 0; c < AT_ONCE; ++c) {
+                const auto* const row = B + static_cast<size_t>(min(n0 + 128 * wave + 16 * (c0 + c) + i, a.N - 1)) * a.r;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) b[c][s] = *reinterpret_cast<const Eight<DT>*>(row + min(32 * s + 8 * g, a.r - 8));
+            }
+#pragma unroll
+            for (int c = 0; c < AT_ONCE; ++c) {
+                v4f x = lowrank_product<DT, STEPS, PIECES>(a.r, g, b[c], piece);
+                if (mine == adapter) {  // an infinity in one request's adapter stays with that request
+                    if constexpr (DT == RCP_F16)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = ldexpf(x[j], E - 14);
+                    *reinterpret_cast<v4f*>(&block[i * ROW + 128 * wave + 16 * (c0 + c) + 4 * g]) = x;
+                }
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        const int row = 4 * y + wave;
+        const bool adds = __shfl(id, row, 64) >= 0;  // uniform
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            if (m0 + row < a.M && n + 4 * p < a.N) {
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (adds) *reinterpret_cast<v4f*>(v) = *reinterpret_cast<const v4f*>(&block[row * ROW + 8 * lane + 4 * p]);
+                lowrank_add4<OUT>(base[y][p], v);
+                lowrank_store4<OUT>(a.out, static_cast<size_t>(m0 + row) * a.N + n + 4 * p, v);
+            }
     }
 }
 
 // ---------------------------------------------------------------------------------------
 struct LowrankPlan {
-    int token_tiles, tiles, chunk, splits, slots, columns;  // token_tiles: sixteens of tokens of a workgroup of the first kernel
+    bool many;
+    int tiles, chunk, splits, slots;  // of the first kernel
 };
 
-static LowrankPlan lowrank_plan(int M, int N, int K)
+static LowrankPlan lowrank_plan(int M, int K)
 {
     LowrankPlan p;
-    p.token_tiles = M > 64 ? 4 : 1;
-    p.tiles = (M + 16 * p.token_tiles - 1) / (16 * p.token_tiles);
+    p.many = M > 64;
+    p.tiles = p.many ? (M + 63) / 64 : (M + 15) / 16;
     const int least = 512, most = (K + least - 1) / least;  // splits of 512 columns and more
-    int splits = 512 / p.tiles;
+    int splits = 2 * num_compute_units() / p.tiles;
     splits = splits < 1 ? 1 : splits > most ? most : splits;
-    p.chunk = ((K + splits - 1) / splits + 127) / 128 * 128;
+    const int unit = p.many ? LOWRANK_STAGE : least;
+    p.chunk = ((K + splits - 1) / splits + unit - 1) / unit * unit;
     p.splits = (K + p.chunk - 1) / p.chunk;
-    p.slots = p.token_tiles > 1 ? 1 : M < 16 ? M : 16;
-    const int tiles16 = (M + 15) / 16, parts = 1024 / tiles16 > 0 ? 1024 / tiles16 : 1;
-    p.columns = ((N + parts - 1) / parts + 127) / 128 * 128;
+    p.slots = p.many ? 4 : M < 16 ? M : 16;
     return p;
 }
 
 size_t lowrank_workspace_bytes(int M, int N, int K, int r)
 {
-    const size_t bytes = static_cast<size_t>(lowrank_plan(M, N, K).splits) * M * r * sizeof(float);
+    const size_t bytes = static_cast<size_t>(lowrank_plan(M, K).splits) * M * r * sizeof(float);
     return bytes > 16 ? bytes : 16;
 }
 
 int launch_lowrank(const void* x, rcp_dtype dt, int M, int N, int K, int r, int adapters, const void* A, const void* B, const int* which,
                    const float* scaling, const void* base, void* out, rcp_dtype out_dt, void* workspace, hipStream_t st)
 {
-    const LowrankPlan p = lowrank_plan(M, N, K);
-    LowrankArgs a = {x, A, B, base, which, scaling, out, static_cast<float*>(workspace), M, N, K, r, adapters, p.splits, p.chunk, p.slots, p.columns};
+    const LowrankPlan p = lowrank_plan(M, K);
+    LowrankArgs a = {x, A, B, base, which, scaling, out, static_cast<float*>(workspace), M, N, K, r, adapters, p.splits, p.chunk, p.slots};
     const dim3 grid(static_cast<unsigned>(p.splits), static_cast<unsigned>(p.slots), static_cast<unsigned>(p.tiles));
-    auto in = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
-    auto form = [&](auto type, auto tokens) {
-        constexpr int DT = decltype(type)::value, TT = decltype(tokens)::value;
-        if (r <= 16) in(&lowrank_in_kernel<DT, TT, 1>);
-        else if (r <= 32) in(&lowrank_in_kernel<DT, TT, 2>);
-        else in(&lowrank_in_kernel<DT, TT, 4>);
+    const unsigned tiles = static_cast<unsigned>((M + 15) / 16);
+    // Many tokens: workgroups go to the eight dies, each with a cache of its own, in turn; with a width of whole eights those that add up the same partial
+    // sums meet on one die.
+    const dim3 grid2 = p.many ? dim3((tiles + 7) / 8 * 8, static_cast<unsigned>((N + LOWRANK_COLUMNS - 1) / LOWRANK_COLUMNS))
+                              : dim3(static_cast<unsigned>((N + 31) / 32), tiles);
+    auto first = [&](auto type, auto ranks) {
+        constexpr int DT = decltype(type)::value, NR = decltype(ranks)::value;
+        if (p.many) enqueue(&lowrank_many_in_kernel<DT, NR>, grid, 256, 0, st, a);
+        else enqueue(&lowrank_few_in_kernel<DT, NR>, grid, 256, 0, st, a);
     };
-    using F16 = std::integral_constant<int, RCP_F16>;
-    using BF16 = std::integral_constant<int, RCP_BF16>;
-    using T1 = std::integral_constant<int, 1>;
-    using T4 = std::integral_constant<int, 4>;
-    if (dt == RCP_F16) p.token_tiles == 4 ? form(F16{}, T4{}) : form(F16{}, T1{});
-    else p.token_tiles == 4 ? form(BF16{}, T4{}) : form(BF16{}, T1{});
-    if (int rc = check_launch("rcp_lowrank_add")) return rc;
-    const dim3 grid2(static_cast<unsigned>((N + p.columns - 1) / p.columns), static_cast<unsigned>((M + 15) / 16));
-    const size_t lds = 16 * ((r + 31) / 32 * 32 + 4) * sizeof(float);
-    auto launch = [&](auto kernel) { enqueue(kernel, grid2, 256, lds, st, a); };
-    auto second = [&](auto type) {
-        constexpr int DT = decltype(type)::value;
-        if (out_dt == RCP_F32) launch(&lowrank_out_kernel<DT, RCP_F32>);
-        else if (out_dt == RCP_F16) launch(&lowrank_out_kernel<DT, RCP_F16>);
-        else launch(&lowrank_out_kernel<DT, RCP_BF16>);
+    auto second = [&](auto type, auto result, auto steps) {
+        constexpr int DT = decltype(type)::value, OUT = decltype(result)::value, STEPS = decltype(steps)::value;
+        if (p.many) enqueue(&lowrank_many_out_kernel<DT, OUT, STEPS>, grid2, 256, 0, st, a);
+        else enqueue(&lowrank_few_out_kernel<DT, OUT, STEPS>, grid2, 256, 0, st, a);
     };
-    if (dt == RCP_F16) second(F16{});
-    else second(BF16{});
-    return check_launch("rcp_lowrank_add(second)");
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    auto result = [&](auto type, auto out_type) {
+        if (r <= 32) second(type, out_type, One{});
+        else if (r <= 64) second(type, out_type, Two{});
+        else second(type, out_type, Four{});
+    };
+    auto form = [&](auto type) {
+        if (r <= 16) first(type, One{});
+        else if (r <= 32) first(type, Two{});
+        else first(type, Four{});
+        if (out_dt == RCP_F32) result(type, std::integral_constant<int, RCP_F32>{});
+        else if (out_dt == RCP_F16) result(type, std::integral_constant<int, RCP_F16>{});
+        else result(type, std::integral_constant<int, RCP_BF16>{});
+    };
+    if (dt == RCP_F16) form(std::integral_constant<int, RCP_F16>{});
+    else form(std::integral_constant<int, RCP_BF16>{});
+    return check_launch("rcp_lowrank_add");
 }
 
 }  // namespace rcp
