@@ -24,6 +24,18 @@ struct Kv8Unit {
     int b, within;
 };
 
+// sum over this lane and those below it
+__device__ __forceinline__ int kv8_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // from the lane before, two, four and eight before in a row of sixteen
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // a row's sum to the next one
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // the first half's to the second
+    return v;
+}
+
 template <class F>
 __device__ __forceinline__ Kv8Unit kv8_find(int sequences, int target, int lane, F count)
 {
@@ -31,12 +43,7 @@ __device__ __forceinline__ Kv8Unit kv8_find(int sequences, int target, int lane,
     for (int base = 0; base < sequences; base += 64) {
         const int b = base + lane;
         const int n = b < sequences ? count(b) : 0;
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(sum, d, 64);
-            if (lane >= d) sum += other;
-        }
+        const int sum = kv8_scan(n);
         const unsigned long long past = __builtin_amdgcn_ballot_w64(before + sum > target);
         if (past != 0) {
             const int at = __builtin_ctzll(past);

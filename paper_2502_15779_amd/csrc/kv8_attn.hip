@@ -37,6 +37,7 @@ struct Kv8AttnArgs {
     const float *k_scales, *v_scales;
     void* out;
     float* part;
+    int2* cut;    // one token a sequence: first chunk and number of chunks of each
     int chunks;   // one token a sequence: chunks of the grid; otherwise splits of the cached tokens
     int tiles;    // several tokens: tiles of rows in the grid
 };
@@ -123,18 +124,10 @@ __device__ __forceinline__ void kv8_to_lds_once(__amdgpu_buffer_rsrc_t from, uns
 }
 
 // ---------------------------------------------------------------------------------------
-// One new token a sequence.  Workgroup = (chunk of cached tokens of a sequence, cache head [, sixteen of its query heads]); the chunks are cut on
-// the device from the lengths, so that a captured call stays balanced when they change.  Wavefront w of the four walks the tiles
-// w, w + 4, ... of 64 tokens on its own.  16x16x32 products: a lane holds the row (query head) lane % 16.
+// One new token a sequence.  Workgroup = one wavefront = (chunk of cached tokens of a sequence, cache head [, sixteen of its query heads]); the chunks are
+// cut on the device from the lengths, so that a captured call stays balanced when they change.  16x16x32 products: a lane holds the row (query
+// head) lane % 16.
 // ---------------------------------------------------------------------------------------
-template <int D>
-struct Kv8DecodeLds {
-    union {
-        unsigned char v[4][KV8_TILE * D];  // a tile's value codes of each wavefront
-        float red[4][16][D];
-    };
-    float m[4][16], l[4][16];
-};
 
 // which 16-byte piece of a token's value codes stands at place p of its row in LDS: p ^ this; the rows that a transposing read takes together
 // (tokens 4g .. 4g + 3 and sixteen further, for two g at a time) fall into different banks
@@ -145,36 +138,92 @@ __device__ __forceinline__ int kv8_decode_swizzle(int token)
     else return ((token >> 4) & 1) | ((token >> 1) & 2);
 }
 
+// Where a workgroup's chunk lies, from the lengths: sequence b (-1: none), its length, its chunk of `tokens` tokens
+struct Kv8Chunk {
+    int b, length, chunk, tokens;
+};
+
+__device__ __forceinline__ Kv8Chunk kv8_chunk(const Kv8Table& t, int chunks, int target, int lane)
+{
+    if (t.sequences == 1) {  // uniform
+        const int n = kv8_clamp(t.lengths[0], 0, t.capacity), C = kv8_chunk_tokens(n, 1, chunks);
+        return {target < kv8_chunks(n, C) ? 0 : -1, n, target, C};
+    }
+    auto length_of = [&](int b) { return kv8_clamp(t.lengths[b], 0, t.capacity); };
+    const int C = kv8_chunk_tokens(kv8_total(t.sequences, lane, length_of), t.sequences, chunks);
+    const Kv8Unit u = kv8_find(t.sequences, target, lane, [&](int b) { return kv8_chunks(length_of(b), C); });
+    if (u.b < 0) return {-1, 0, 0, C};
+    const int b = __builtin_amdgcn_readfirstlane(u.b);
+    return {b, __builtin_amdgcn_readfirstlane(length_of(b)), __builtin_amdgcn_readfirstlane(u.within), C};
+}
+
 template <int D, int QP, int PP>
-__global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
+__global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 {
     constexpr int KX = D / 64;  // 16-byte loads of a lane for sixteen tokens' keys
-    __shared__ Kv8DecodeLds<D> lds;
-    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ __attribute__((aligned(16))) unsigned char values[KV8_TILE * D];  // a tile's value codes
+    const int lane = threadIdx.x, i = lane & 15, g = lane >> 4;
     const int chunk = static_cast<int>(blockIdx.x) / a.H_kv, hk = static_cast<int>(blockIdx.x) - chunk * a.H_kv;
-    auto length_of = [&](int b) { return kv8_clamp(a.t.lengths[b], 0, a.t.capacity); };
-    const int total = kv8_total(a.t.sequences, lane, length_of);
-    const int C = kv8_chunk_tokens(total, a.t.sequences, a.chunks, KV8_TILE);
-    const Kv8Unit u = kv8_find(a.t.sequences, chunk, lane, [&](int b) { return kv8_chunks(length_of(b), C); });
-    if (u.b < 0) return;
-    const int b = __builtin_amdgcn_readfirstlane(u.b), t0 = __builtin_amdgcn_readfirstlane(u.within) * C;
-    const int len = __builtin_amdgcn_readfirstlane(length_of(b)), t_end = min(len, t0 + C);
+    const Kv8Chunk at = kv8_chunk(a.t, a.chunks, chunk, lane);
+    if (at.b < 0) return;
+    const int b = at.b, len = at.length, t0 = at.chunk * at.tokens, t_end = min(len, t0 + at.tokens);
     const int R = min(16, a.rep - static_cast<int>(blockIdx.y) * 16);
     const int h0 = hk * a.rep + static_cast<int>(blockIdx.y) * 16;
-    const int first = t0 + KV8_TILE * wave;
-    const int tiles = t_end > first ? (t_end - first + 4 * KV8_TILE - 1) / (4 * KV8_TILE) : 0;
-    const int* const row = a.t.table + static_cast<size_t>(b) * a.t.width;
+    const int tiles = t_end > t0 ? (t_end - t0 + KV8_TILE - 1) / KV8_TILE : 0;
+    const int of = kv8_chunks(len, at.tokens);
+    if (at.chunk == 0 && hk == 0 && blockIdx.y == 0 && lane == 0) a.cut[b] = make_int2(chunk, of);  // for the merge
+
+    // pages and scales of sixteen tiles: lane = sixteen tokens
+    int page;
+    float k_scale, v_scale;
+    auto look_up = [&](int base) {
+        const int pos = base + 16 * lane;
+        page = pos < t_end ? kv8_page(a.t, a.t.table + static_cast<size_t>(b) * a.t.width, pos) : -1;
+        const size_t s = static_cast<size_t>(max(page, 0)) * a.H_kv + hk;
+        k_scale = a.k_scales[s];
+        v_scale = a.v_scales[s];
+    };
+    auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
+    };
+    auto block_of = [&](int base, int in, int n) {  // tile `in` of those looked up
+        return kv8_block(a.t, a.H_kv, hk, __builtin_amdgcn_readlane(page, 4 * in + n), base + 16 * n, t_end);
+    };
+    u32x4 kw[4][KX];
+    auto load_keys = [&](int base, int in) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const __amdgpu_buffer_rsrc_t kr = resource(a.k_codes, block_of(base, in, n));
+#pragma unroll
+            for (int x = 0; x < KX; ++x) kw[n][x] = __builtin_amdgcn_raw_buffer_load_b128(kr, i * D + 16 * g + 64 * x, 0, 2);
+        }
+    };
+    auto load_values = [&](int base, int in) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const __amdgpu_buffer_rsrc_t vr = resource(a.v_codes, block_of(base, in, n));
+#pragma unroll
+            for (int y = 0; y < KX; ++y) {
+                constexpr int P = D / 16;  // pieces a token
+                const int s16 = 64 * y + lane, token = s16 / P, place = s16 % P;
+                kv8_to_lds_once(vr, &values[16 * n * D + 1024 * y], token * D + ((place ^ kv8_decode_swizzle<D>(16 * n + token)) * 16));
+            }
+        }
+    };
 
     // ---- the query: lane = (head i, the elements of the key pieces 16 g .. of each 64) ----
     v8h qh[2 * KX], ql[QP == 2 ? 2 * KX : 1];
-    float unit;
-    {
+    float unit = 0.0f;
+    if (tiles > 0) {
         float t[2 * KX][8];
-        const size_t at = (static_cast<size_t>(b) * a.H_q + h0 + min(i, R - 1)) * D + 16 * g;
+        const size_t from = (static_cast<size_t>(b) * a.H_q + h0 + min(i, R - 1)) * D + 16 * g;
         float top = 0.0f;
 #pragma unroll
-        for (int d = 0; d < 2 * KX; ++d) kv8_query8(a, at + 64 * (d >> 1) + 8 * (d & 1), t[d]);
+        for (int d = 0; d < 2 * KX; ++d) kv8_query8(a, from + 64 * (d >> 1) + 8 * (d & 1), t[d]);
+        look_up(t0);
+        load_keys(t0, 0);
+        load_values(t0, 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int d = 0; d < 2 * KX; ++d)
 #pragma unroll
@@ -191,41 +240,12 @@ __global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
         unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
     }
 
-    auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
-    };
-    u32x4 kw[4][KX];
-    float ks[4], vs[4];
-    bool page[4];
-    auto load_tile = [&](int base) {  // keys into registers, values into LDS
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const int pos = base + 16 * n;
-            const int id = __builtin_amdgcn_readfirstlane(pos < t_end ? kv8_page(a.t, row, pos) : -1);
-            page[n] = id >= 0;
-            const size_t s = static_cast<size_t>(max(id, 0)) * a.H_kv + hk;
-            ks[n] = a.k_scales[s];
-            vs[n] = a.v_scales[s];
-            const Kv8Block block = kv8_block(a.t, a.H_kv, hk, id, pos, t_end);
-            const __amdgpu_buffer_rsrc_t kr = resource(a.k_codes, block), vr = resource(a.v_codes, block);
-#pragma unroll
-            for (int x = 0; x < KX; ++x) kw[n][x] = __builtin_amdgcn_raw_buffer_load_b128(kr, i * D + 16 * g + 64 * x, 0, 2);
-#pragma unroll
-            for (int y = 0; y < KX; ++y) {
-                constexpr int P = D / 16;  // pieces a token
-                const int s16 = 64 * y + lane, token = s16 / P, at = s16 % P;
-                kv8_to_lds_once(vr, &lds.v[wave][16 * n * D + 1024 * y], token * D + ((at ^ kv8_decode_swizzle<D>(16 * n + token)) * 16));
-            }
-        }
-    };
-
     v4f acc[D / 16];
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) acc[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = KV8_LOW, l = 0.0f;
     for (int c = 0; c < tiles; ++c) {
-        const int base = first + 4 * KV8_TILE * c;
-        load_tile(base);
+        const int base = t0 + KV8_TILE * c, in = c & 15;
         v4f S[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
@@ -237,16 +257,30 @@ __global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
                 S[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qh[d], S[n], 0, 0, 0);
             }
         }
-        float sc[4][4], top = -INFINITY;
-        const bool whole = base + KV8_TILE <= t_end && page[0] && page[1] && page[2] && page[3];
+        float ks[4], vs[4];
+        bool there[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            const float by = ks[n] * unit;
+            ks[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scale), 4 * in + n)) * unit;
+            vs[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scale), 4 * in + n));
+            there[n] = __builtin_amdgcn_readlane(page, 4 * in + n) >= 0;
+        }
+        const bool more = c + 1 < tiles;  // uniform
+        if (more) {
+            if (in == 15) look_up(base + KV8_TILE);
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(base + KV8_TILE, (c + 1) & 15);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        float sc[4][4], top = -INFINITY;
+        const bool whole = base + KV8_TILE <= t_end && there[0] && there[1] && there[2] && there[3];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[n][j] = S[n][j] * by;
+        for (int n = 0; n < 4; ++n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[n][j] = S[n][j] * ks[n];
             if (!whole) {  // uniform
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sc[n][j] = page[n] && base + 16 * n + 4 * g + j < t_end ? sc[n][j] : -INFINITY;
+                for (int j = 0; j < 4; ++j) sc[n][j] = there[n] && base + 16 * n + 4 * g + j < t_end ? sc[n][j] : -INFINITY;
             }
             top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])) + kv8_log_scale(vs[n]));
         }
@@ -273,19 +307,21 @@ __global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
             ph[s] = kv8_round(w);
             if constexpr (PP == 2) pl[s] = kv8_rest(w, ph[s]);
         }
+        // the values of this tile are in LDS once no more loads than the keys requested above are outstanding
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // the values are in LDS
+        if (more) __builtin_amdgcn_s_waitcnt((4 * KX) | (7 << 4) | (15 << 8));
+        else __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
         __builtin_amdgcn_sched_barrier(0);
         const int r = i >> 1;
         const int token = 16 * (r >> 2) + 4 * g + (r & 3);
-        const unsigned char* const at = &lds.v[wave][0] + token * D + (i & 1) * 8;
+        const unsigned char* const vat = &values[token * D + (i & 1) * 8];
         const int f = kv8_decode_swizzle<D>(token);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (__attribute__((address_space(3))) v2i*)(at + 32 * s * D + ((d ^ f) * 16)));
+                    (__attribute__((address_space(3))) v2i*)(vat + 32 * s * D + ((d ^ f) * 16)));
                 const v8h v = kv8_halves(static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]));
                 if constexpr (PP == 2) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[s], acc[d], 0, 0, 0);
                 acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[s], acc[d], 0, 0, 0);
@@ -293,74 +329,58 @@ __global__ __launch_bounds__(256) void kv8_decode_kernel(Kv8AttnArgs a)
         // every read of the tile has returned before the next one overwrites it
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+        if (more) load_values(base + KV8_TILE, (c + 1) & 15);
         __builtin_amdgcn_sched_barrier(0);
     }
     l = fold32f(fold16f(l, l), fold16f(l, l));
-    __syncthreads();  // LDS changes hands
-    if (i < R) {
+    if (i >= R) return;
+    const int h = h0 + i;
+    if (of == 1) {
+        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+        const size_t to = (static_cast<size_t>(b) * a.H_q + h) * D + 4 * g;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<v4f*>(&lds.red[wave][i][16 * d + 4 * g]) = acc[d];
-        if (g == 0) {
-            lds.m[wave][i] = m;
-            lds.l[wave][i] = l;
-        }
-    }
-    __syncthreads();
-    const bool alone = kv8_chunks(len, C) == 1;
-    for (int idx = tid; idx < R * D; idx += 256) {
-        const int h = idx / D, j = idx % D;
-        float M = lds.m[0][h];
+        for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int w = 1; w < 4; ++w) M = fmaxf(M, lds.m[w][h]);
-        float sum = 0.0f, ls = 0.0f;
+            for (int j = 0; j < 4; ++j) kv8_put(a.out, a.out_dt, to + 16 * d + j, l == 0.0f ? 0.0f : acc[d][j] * by);
+    } else {
+        float* const dst = a.part + (static_cast<size_t>(chunk) * a.H_q + h) * (D + KV8_EXTRA);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float e = __builtin_amdgcn_exp2f(lds.m[w][h] - M);
-            sum = fmaf(e, lds.red[w][h][j], sum);
-            ls = fmaf(e, lds.l[w][h], ls);
-        }
-        if (alone) kv8_put(a.out, a.out_dt, (static_cast<size_t>(b) * a.H_q + h0 + h) * D + j, ls == 0.0f ? 0.0f : sum / ls);
-        else {
-            float* const dst = a.part + (static_cast<size_t>(chunk) * a.H_q + h0 + h) * (D + KV8_EXTRA);
-            dst[j] = sum;
-            if (j == 0) {
-                dst[D] = M;
-                dst[D + 1] = ls;
-            }
-        }
+        for (int d = 0; d < D / 16; ++d) *reinterpret_cast<v4f*>(dst + 16 * d + 4 * g) = acc[d];
+        if (g == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(m, l);
     }
 }
 
-// Merges n partial results `stride` floats apart into one row: thread (part, j) of `groups` x D takes every groups-th of them.
-template <int D>
+// Merges n partial results `stride` floats apart into one row: thread (g, j) of GROUPS x D takes element j of every GROUPS-th of them, eight at a
+// time so that their loads are under way together.
+template <int D, int GROUPS>
 __device__ __forceinline__ void kv8_merge(const float* src, size_t stride, int n, void* out, int out_dt, size_t row)
 {
-    constexpr int GROUPS = 512 / D;
+    constexpr int U = 8;
     __shared__ float red[GROUPS][D], dred[GROUPS], mred[GROUPS];
     const int j = threadIdx.x % D, g = threadIdx.x / D;
     float M = KV8_LOW, num = 0.0f, den = 0.0f;
-    for (int i0 = g; i0 < n; i0 += 4 * GROUPS) {
-        float mi[4], li[4], ai[4];
+    for (int i0 = g; i0 < n; i0 += U * GROUPS) {
+        float2 ml[U];
+        float v[U];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
+        for (int x = 0; x < U; ++x) {
             const float* const s = src + static_cast<size_t>(min(i0 + GROUPS * x, n - 1)) * stride;
-            mi[x] = s[D];
-            li[x] = s[D + 1];
-            ai[x] = s[j];
+            ml[x] = *reinterpret_cast<const float2*>(s + D);
+            v[x] = s[j];
         }
         float mb = M;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-            if (i0 + GROUPS * x < n) mb = fmaxf(mb, mi[x]);
+        for (int x = 0; x < U; ++x)
+            if (i0 + GROUPS * x < n) mb = fmaxf(mb, ml[x].x);
         const float r = __builtin_amdgcn_exp2f(M - mb);
         num *= r;
         den *= r;
         M = mb;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const float e = i0 + GROUPS * x < n ? __builtin_amdgcn_exp2f(mi[x] - M) : 0.0f;
-            num = fmaf(e, ai[x], num);
-            den = fmaf(e, li[x], den);
+        for (int x = 0; x < U; ++x) {
+            const float e = i0 + GROUPS * x < n ? __builtin_amdgcn_exp2f(ml[x].x - M) : 0.0f;
+            num = fmaf(e, v[x], num);
+            den = fmaf(e, ml[x].y, den);
         }
     }
     red[g][j] = num;
@@ -385,17 +405,14 @@ __device__ __forceinline__ void kv8_merge(const float* src, size_t stride, int n
 }
 
 // blockIdx = (query head, sequence): the chunks of a sequence that has more than one
-template <int D>
-__global__ __launch_bounds__(512) void kv8_decode_merge_kernel(Kv8AttnArgs a)
+template <int D, int GROUPS>
+__global__ __launch_bounds__(GROUPS * D) void kv8_decode_merge_kernel(Kv8AttnArgs a)
 {
-    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63;
-    auto length_of = [&](int x) { return kv8_clamp(a.t.lengths[x], 0, a.t.capacity); };
-    const int C = kv8_chunk_tokens(kv8_total(a.t.sequences, lane, length_of), a.t.sequences, a.chunks, KV8_TILE);
-    const int n = kv8_chunks(length_of(b), C);
-    if (n == 1) return;  // the attention kernel has written it
-    const int before = kv8_total(b, lane, [&](int x) { return kv8_chunks(length_of(x), C); });
-    kv8_merge<D>(a.part + (static_cast<size_t>(before) * a.H_q + h) * (D + KV8_EXTRA), static_cast<size_t>(a.H_q) * (D + KV8_EXTRA), n, a.out, a.out_dt,
-                 static_cast<size_t>(b) * a.H_q + h);
+    const int h = blockIdx.x, b = blockIdx.y;
+    const int2 cut = a.cut[b];
+    if (cut.y == 1) return;  // the attention kernel has written it
+    kv8_merge<D, GROUPS>(a.part + (static_cast<size_t>(cut.x) * a.H_q + h) * (D + KV8_EXTRA), static_cast<size_t>(a.H_q) * (D + KV8_EXTRA), cut.y, a.out,
+                         a.out_dt, static_cast<size_t>(b) * a.H_q + h);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -597,13 +614,13 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 }
 
 // blockIdx = (query head, row of the call)
-template <int D>
-__global__ __launch_bounds__(512) void kv8_prompt_merge_kernel(Kv8AttnArgs a)
+template <int D, int GROUPS>
+__global__ __launch_bounds__(GROUPS * D) void kv8_prompt_merge_kernel(Kv8AttnArgs a)
 {
     const int h = blockIdx.x, t = blockIdx.y;
     if (kv8_sequence_of(a.t.starts, a.t.sequences, t, a.rows) < 0) return;
     const size_t row = static_cast<size_t>(t) * a.H_q + h, stride = static_cast<size_t>(a.rows) * a.H_q * (D + KV8_EXTRA);
-    kv8_merge<D>(a.part + row * (D + KV8_EXTRA), stride, a.chunks, a.out, a.out_dt, row);
+    kv8_merge<D, GROUPS>(a.part + row * (D + KV8_EXTRA), stride, a.chunks, a.out, a.out_dt, row);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -620,9 +637,9 @@ static Kv8AttnPlan kv8_attn_plan(int rows, int sequences, int H_q, int H_kv, int
     const int cus = num_compute_units(), rep = H_q / H_kv;
     const size_t partial = static_cast<size_t>(H_q) * (D + KV8_EXTRA) * sizeof(float);
     if (one) {
-        p.chunks = 4 * cus / H_kv > 2 * sequences ? 4 * cus / H_kv : 2 * sequences;
+        p.chunks = 8 * cus / H_kv > 2 * sequences ? 8 * cus / H_kv : 2 * sequences;
         p.tiles = 0;
-        p.bytes = static_cast<size_t>(p.chunks) * partial;
+        p.bytes = static_cast<size_t>(p.chunks) * partial + sequences * sizeof(int2);
     } else {
         p.tiles = static_cast<int>(static_cast<long long>(rows) * rep / KV8_ROWS) + sequences;
         const long long groups = static_cast<long long>(p.tiles) * H_kv;
@@ -662,6 +679,7 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
     a.v_scales = c.v_scales;
     a.out = c.out;
     a.part = static_cast<float*>(c.workspace);
+    a.cut = reinterpret_cast<int2*>(a.part + static_cast<size_t>(plan.chunks) * c.H_q * (c.D + KV8_EXTRA));
     a.chunks = plan.chunks;
     a.tiles = plan.tiles;
     const bool q2 = c.q_dtype == RCP_F32;
@@ -669,7 +687,7 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
         constexpr int D = decltype(size)::value;
         if (one) {
             const dim3 grid(static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv), static_cast<unsigned>((a.rep + 15) / 16));
-            auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
+            auto launch = [&](auto kernel) { enqueue(kernel, grid, 64, 0, st, a); };
             const bool p2 = c.out_dtype != RCP_BF16;
             if (q2 && p2) launch(&kv8_decode_kernel<D, 2, 2>);
             else if (q2) launch(&kv8_decode_kernel<D, 2, 1>);
@@ -690,9 +708,21 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
     if (int rc = check_launch("rcp_kv8_attn")) return rc;
     if (!one && plan.chunks == 1) return RCP_OK;
     const dim3 grid(static_cast<unsigned>(c.H_q), static_cast<unsigned>(one ? c.sequences : c.rows));
-    auto merge = [&](auto kernel) { enqueue(kernel, grid, 512, 0, st, a); };
-    if (one) c.D == 128 ? merge(&kv8_decode_merge_kernel<128>) : merge(&kv8_decode_merge_kernel<64>);
-    else c.D == 128 ? merge(&kv8_prompt_merge_kernel<128>) : merge(&kv8_prompt_merge_kernel<64>);
+    // wavefronts for the partial results of a row: eight to a thread at a time
+    auto merge = [&](auto size) {
+        constexpr int D = decltype(size)::value;
+        const int each = one ? plan.chunks / c.sequences : plan.chunks;
+        auto launch = [&](auto groups) {
+            constexpr int G = decltype(groups)::value;
+            if (one) enqueue(&kv8_decode_merge_kernel<D, G>, grid, G * D, 0, st, a);
+            else enqueue(&kv8_prompt_merge_kernel<D, G>, grid, G * D, 0, st, a);
+        };
+        if (each <= 16) launch(std::integral_constant<int, 128 / D>{});
+        else if (each <= 32) launch(std::integral_constant<int, 256 / D>{});
+        else launch(std::integral_constant<int, 1024 / D>{});
+    };
+    if (c.D == 128) merge(std::integral_constant<int, 128>{});
+    else merge(std::integral_constant<int, 64>{});
     return check_launch("rcp_kv8_attn(merge)");
 }
 

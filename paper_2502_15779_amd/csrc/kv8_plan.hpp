@@ -57,18 +57,20 @@ RCP_BOTH long long kv8_most_pages(int rows, int sequences, int shift)
     return (static_cast<long long>(rows) >> shift) + 2LL * sequences;
 }
 
-// Tokens per chunk of the attention of one token a sequence: the fewest, in whole tiles of `unit`, with which `total` cached tokens of `sequences`
-// sequences make at most `chunks` chunks (chunks >= 2 * sequences): sum ceil(n / C) <= total / C + sequences.
-RCP_BOTH int kv8_chunk_tokens(long long total, int sequences, int chunks, int unit)
+// Tokens per chunk of the attention of one token a sequence: the fewest, in whole tiles of 64, with which `total` cached tokens (below 2^31) of
+// `sequences` sequences make at most `chunks` chunks (chunks >= 2 * sequences): sum ceil(n / C) <= total / C + sequences.
+RCP_BOTH int kv8_chunk_tokens(int total, int sequences, int chunks)
 {
-    const long long room = chunks - sequences;
-    const long long c = (total + room - 1) / room;
-    const long long tokens = (c + unit - 1) / unit * unit;
-    return static_cast<int>(tokens < unit ? unit : tokens);
+    const unsigned room = static_cast<unsigned>(chunks - sequences);
+    const unsigned c = (static_cast<unsigned>(total) + room - 1) / room;
+    return c <= 64 ? 64 : static_cast<int>((c + 63) / 64 * 64);
 }
 
 // chunks of a sequence: an empty one has one too, which writes zeros
-RCP_BOTH int kv8_chunks(int tokens, int per_chunk) { return tokens <= 0 ? 1 : (tokens + per_chunk - 1) / per_chunk; }
+RCP_BOTH int kv8_chunks(int tokens, int per_chunk)
+{
+    return tokens <= 0 ? 1 : static_cast<int>((static_cast<unsigned>(tokens) + static_cast<unsigned>(per_chunk) - 1) / static_cast<unsigned>(per_chunk));
+}
 
 // The sequence whose run holds row t, -1 if none does: the last b with starts[b] <= t.  Ends for any contents of `starts`.
 RCP_BOTH int kv8_sequence_of(const int* starts, int sequences, int t, int rows)

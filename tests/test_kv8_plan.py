@@ -30,7 +30,7 @@ int main()
         }
         long long total = 0;
         for (int v : lengths) total += kv8_clamp(v, 0, width << shift);
-        const int C = kv8_chunk_tokens(total, n, chunks, 64);
+        const int C = kv8_chunk_tokens(static_cast<int>(total), n, chunks);
         long long sum = 0;
         for (int v : lengths) sum += kv8_chunks(kv8_clamp(v, 0, width << shift), C);
         printf("| %lld %lld %d %lld |", pages, kv8_most_pages(rows, n, shift), C, sum);
