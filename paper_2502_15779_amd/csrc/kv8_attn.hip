@@ -91,8 +91,8 @@ __device__ __forceinline__ void kv8_put(void* out, int dt, size_t i, float v)
     else static_cast<__bf16*>(out)[i] = static_cast<__bf16>(v);
 }
 
-// log2 of a page's scale as the weights' reference takes it: scales are 2^-40 .. 2^120, and a page that was never written has 0
-__device__ __forceinline__ float kv8_log_scale(float s) { return __builtin_amdgcn_logf(__builtin_amdgcn_fmed3f(s, 0x1p-40f, 0x1p120f)); }
+// Scales are 2^-40 .. 2^120, and a page that was never written has 0 (and zeros for codes): as a weight's factor, the nearest of those.
+constexpr float KV8_LEAST = 0x1p-40f, KV8_MOST = 0x1p120f;
 
 // the page that holds position `pos` of sequence b, -1 where there is none
 __device__ __forceinline__ int kv8_page(const Kv8Table& t, const int* row, int pos)
@@ -109,7 +109,9 @@ struct Kv8Block {
 };
 __device__ __forceinline__ Kv8Block kv8_block(const Kv8Table& t, int H, int h, int id, int pos, int end)
 {
-    return {((static_cast<size_t>(max(id, 0)) * H + h) << t.shift) + (pos & ((1 << t.shift) - 1)), id < 0 ? 0 : kv8_clamp(end - pos, 0, 16)};
+    // (uniform, and in scalar registers: a buffer's bounds in vector registers would be a loop over their values)
+    return {((static_cast<size_t>(max(id, 0)) * H + h) << t.shift) + (pos & ((1 << t.shift) - 1)),
+            __builtin_amdgcn_readfirstlane(id < 0 ? 0 : kv8_clamp(end - pos, 0, 16))};
 }
 
 // 16 bytes of a lane from a buffer straight into LDS, lane after lane from `to` on (a function of its own: inside a template, the host's
@@ -175,13 +177,15 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 
     // pages and scales of sixteen tiles: lane = sixteen tokens
     int page;
-    float k_scale, v_scale;
+    float k_scale, v_inverse, v_log;
     auto look_up = [&](int base) {
         const int pos = base + 16 * lane;
         page = pos < t_end ? kv8_page(a.t, a.t.table + static_cast<size_t>(b) * a.t.width, pos) : -1;
         const size_t s = static_cast<size_t>(max(page, 0)) * a.H_kv + hk;
         k_scale = a.k_scales[s];
-        v_scale = a.v_scales[s];
+        const float v_scale = __builtin_amdgcn_fmed3f(a.v_scales[s], KV8_LEAST, KV8_MOST);
+        v_inverse = 1.0f / v_scale;
+        v_log = __builtin_amdgcn_logf(v_scale);
     };
     auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
@@ -257,12 +261,13 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
                 S[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qh[d], S[n], 0, 0, 0);
             }
         }
-        float ks[4], vs[4];
+        float ks[4], vs[4], ls[4];
         bool there[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             ks[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scale), 4 * in + n)) * unit;
-            vs[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_scale), 4 * in + n));
+            vs[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_inverse), 4 * in + n));
+            ls[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_log), 4 * in + n));
             there[n] = __builtin_amdgcn_readlane(page, 4 * in + n) >= 0;
         }
         const bool more = c + 1 < tiles;  // uniform
@@ -272,17 +277,15 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
             load_keys(base + KV8_TILE, (c + 1) & 15);
         }
         __builtin_amdgcn_sched_barrier(0);
-        float sc[4][4], top = -INFINITY;
+        float top = -INFINITY;
         const bool whole = base + KV8_TILE <= t_end && there[0] && there[1] && there[2] && there[3];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sc[n][j] = S[n][j] * ks[n];
             if (!whole) {  // uniform
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sc[n][j] = there[n] && base + 16 * n + 4 * g + j < t_end ? sc[n][j] : -INFINITY;
+                for (int j = 0; j < 4; ++j) S[n][j] = there[n] && base + 16 * n + 4 * g + j < t_end ? S[n][j] : -INFINITY;
             }
-            top = fmaxf(top, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])) + kv8_log_scale(vs[n]));
+            top = fmaxf(top, fmaf(fmaxf(fmaxf(fmaxf(S[n][0], S[n][1]), S[n][2]), S[n][3]), ks[n], ls[n]));
         }
         if (__builtin_amdgcn_ballot_w64(top > m + KV8_TOP) != 0) {
             const float t = kv8_swap32_max(kv8_swap16_max(top));
@@ -300,10 +303,10 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int n = 2 * s + (e >> 2);
-                const float p = __builtin_amdgcn_exp2f(sc[n][e & 3] - m);
-                l += p;
-                w[e] = p * vs[n];
+                w[e] = __builtin_amdgcn_exp2f(fmaf(S[n][e & 3], ks[n], ls[n] - m));
             }
+            l = fmaf((w[0] + w[1]) + (w[2] + w[3]), vs[2 * s], l);
+            l = fmaf((w[4] + w[5]) + (w[6] + w[7]), vs[2 * s + 1], l);
             ph[s] = kv8_round(w);
             if constexpr (PP == 2) pl[s] = kv8_rest(w, ph[s]);
         }
@@ -421,6 +424,7 @@ __global__ __launch_bounds__(GROUPS * D) void kv8_decode_merge_kernel(Kv8AttnArg
 // wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS.
 // ---------------------------------------------------------------------------------------
 constexpr int KV8_ROWS = 128;
+constexpr int KV8_STAGES = 4;  // tiles in LDS: one in use, the others under way
 
 template <int D>
 __device__ __forceinline__ int kv8_prompt_swizzle(int token)
@@ -433,8 +437,7 @@ template <int D, int QP, int PP>
 __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 {
     constexpr int KL = D / 32, DB = D / 32, P = D / 16, LOADS = D / 64;
-    __shared__ unsigned char kt[2][KV8_TILE * D], vt[2][KV8_TILE * D];
-    __shared__ float4 info[2][4];  // of sixteen tokens: key scale, value scale, its logarithm, 1 where there is a page
+    __shared__ __attribute__((aligned(16))) unsigned char kt[KV8_STAGES][KV8_TILE * D], vt[KV8_STAGES][KV8_TILE * D];
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int rest = blockIdx.x;
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
     const int n_rows = __builtin_amdgcn_readfirstlane(run.count) * a.rep;
     const int len = min(__builtin_amdgcn_readfirstlane(run.length), a.t.capacity);
     auto sees = [&](int r) { return kv8_clamp(pos0 + min(r, n_rows - 1) / a.rep + 1, 0, len); };  // tokens that row r may see
-    const int wg_sees = sees(row0 + KV8_ROWS - 1);
+    const int wg_sees = __builtin_amdgcn_readfirstlane(sees(row0 + KV8_ROWS - 1));
     const int all_tiles = (wg_sees + KV8_TILE - 1) / KV8_TILE, per = (all_tiles + a.chunks - 1) / a.chunks;
     const int tile0 = split * per, tile1 = min(all_tiles, tile0 + per);
     const int my = row0 + 32 * wave + c, limit = sees(my);
@@ -489,9 +492,16 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
     auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes) + x.at * D, 0, x.tokens * D, 0x00020000);
     };
-    auto stage = [&](int tile, int buf) {  // sixteen tokens of the tile by each wavefront
-        const int pos = tile * KV8_TILE + 16 * wave;
-        const int id = __builtin_amdgcn_readfirstlane(pos < wg_sees ? kv8_page(a.t, table, pos) : -1);
+    // pages and scales of sixteen tiles: lane = sixteen tokens
+    int page = -1, ahead = -1;
+    float k_scale, v_inverse, v_log;
+    auto look_up = [&](int tile) {
+        const int pos = tile * KV8_TILE + 16 * lane;
+        return pos < wg_sees && tile + (lane >> 2) < tile1 ? kv8_page(a.t, table, pos) : -1;
+    };
+    auto stage = [&](int tile) {  // sixteen tokens of the tile by each wavefront; beyond the last tile: nothing, but as many loads
+        const int in = tile - tile0, buf = in % KV8_STAGES, pos = tile * KV8_TILE + 16 * wave;
+        const int id = __builtin_amdgcn_readlane(ahead, 4 * (in & 15) + wave);
         const Kv8Block block = kv8_block(a.t, a.H_kv, hk, id, pos, wg_sees);
         const __amdgpu_buffer_rsrc_t kr = resource(a.k_codes, block), vr = resource(a.v_codes, block);
 #pragma unroll
@@ -501,9 +511,6 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             kv8_to_lds(kr, &kt[buf][16 * wave * D + 1024 * y], from);
             kv8_to_lds(vr, &vt[buf][16 * wave * D + 1024 * y], from);
         }
-        const size_t s = static_cast<size_t>(max(id, 0)) * a.H_kv + hk;
-        const float vscale = a.v_scales[s];
-        if (lane == 0) info[buf][wave] = make_float4(a.k_scales[s], vscale, kv8_log_scale(vscale), id >= 0 ? 1.0f : 0.0f);
     };
 
     v16f acc[DB];
@@ -512,12 +519,29 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
     float m = KV8_LOW, l = 0.0f;
-    if (tile0 < tile1) stage(tile0, 0);
+    if (tile0 < tile1) {
+        ahead = look_up(tile0);
+#pragma unroll
+        for (int x = 0; x < KV8_STAGES - 1; ++x) stage(tile0 + x);
+    }
     for (int tile = tile0; tile < tile1; ++tile) {
-        const int buf = (tile - tile0) & 1, base = tile * KV8_TILE;
-        __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the tile is in LDS,
-        __syncthreads();                // everybody's is, and the other buffer has been read
-        if (tile + 1 < tile1) stage(tile + 1, buf ^ 1);
+        const int in = tile - tile0, buf = in % KV8_STAGES, base = tile * KV8_TILE;
+        if ((in & 15) == 0) {  // uniform
+            page = look_up(tile);
+            const size_t s = static_cast<size_t>(max(page, 0)) * a.H_kv + hk;
+            const float v_scale = __builtin_amdgcn_fmed3f(a.v_scales[s], KV8_LEAST, KV8_MOST);
+            k_scale = a.k_scales[s];
+            v_inverse = 1.0f / v_scale;
+            v_log = __builtin_amdgcn_logf(v_scale);
+        }
+        if (((in + KV8_STAGES - 1) & 15) == 0) ahead = look_up(tile + KV8_STAGES - 1);
+        // this wavefront's part of the tile is in LDS once only the later tiles' loads are outstanding,
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((2 * LOADS * (KV8_STAGES - 2)) | (7 << 4) | (15 << 8));
+        __syncthreads();  // then everybody's is, and the tile before has been read
+        __builtin_amdgcn_sched_barrier(0);
+        stage(tile + KV8_STAGES - 1);
+        __builtin_amdgcn_sched_barrier(0);
         if (base >= wave_most) continue;  // uniform over the wavefront: none of its rows sees the tile
         v16f S[2];
 #pragma unroll
@@ -539,23 +563,33 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
                 S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k][1], S[tb], 0, 0, 0);
             }
         }
-        float4 page[4];
+        float ks[4], vi[4], vl[4];
+        bool there[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) page[n] = info[buf][n];
-        const bool whole = base + KV8_TILE <= wave_least && page[0].w + page[1].w + page[2].w + page[3].w == 4.0f;
-        float top = -INFINITY;
+        for (int n = 0; n < 4; ++n) {
+            const int at = 4 * (in & 15) + n;
+            there[n] = __builtin_amdgcn_readlane(page, at) >= 0;
+            ks[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k_scale), at));
+            vi[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_inverse), at));
+            vl[n] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_log), at));
+        }
+        const bool whole = base + KV8_TILE <= wave_least && there[0] && there[1] && there[2] && there[3];
+        // sixteen tokens of a page are eight scores of a lane: score = S by[n], weight = 2^(score + log2 s' - m) in one multiply-add and one exponential
+        float by[4], top = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {  // sixteen tokens: eight scores of a lane
-            const float by = page[n].x * unit;
-            float most = -INFINITY;
+        for (int n = 0; n < 4; ++n) {
+            by[n] = ks[n] * unit;
+            if (!whole) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float x = S[n >> 1][8 * (n & 1) + e] * by;
-                if (!whole) x = page[n].w != 0.0f && base + 16 * n + 8 * (e >> 2) + 4 * hh + (e & 3) < limit ? x : -INFINITY;
-                S[n >> 1][8 * (n & 1) + e] = x;
-                most = fmaxf(most, x);
+                for (int e = 0; e < 8; ++e) {
+                    const bool seen = there[n] && base + 16 * n + 8 * (e >> 2) + 4 * hh + (e & 3) < limit;
+                    S[n >> 1][8 * (n & 1) + e] = seen ? S[n >> 1][8 * (n & 1) + e] : -INFINITY;
+                }
             }
-            top = fmaxf(top, most + page[n].z);
+            const v16f& x = S[n >> 1];
+            const int o = 8 * (n & 1);
+            const float most = fmaxf(fmaxf(fmaxf(x[o], x[o + 1]), x[o + 2]), fmaxf(fmaxf(x[o + 3], x[o + 4]), fmaxf(fmaxf(x[o + 5], x[o + 6]), x[o + 7])));
+            top = fmaxf(top, fmaf(most, by[n], vl[n]));
         }
         if (__builtin_amdgcn_ballot_w64(top > m + KV8_TOP) != 0) {
             const float t = kv8_swap32_max(top);
@@ -572,12 +606,10 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float w[8];
+            const float less = vl[n] - m;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float p = __builtin_amdgcn_exp2f(S[n >> 1][8 * (n & 1) + e] - m);
-                l += p;
-                w[e] = p * page[n].y;
-            }
+            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(S[n >> 1][8 * (n & 1) + e], by[n], less));
+            l = fmaf(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])), vi[n], l);
             const v8h ph = kv8_round(w);
             v8h pl;
             if constexpr (PP == 2) pl = kv8_rest(w, ph);
@@ -591,6 +623,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             }
         }
     }
+    __builtin_amdgcn_s_waitcnt(0);  // nothing is on its way into LDS any more
     l = fold32f(l, l);
     if (my >= n_rows) return;
     if (a.chunks == 1) {
