@@ -433,6 +433,24 @@ __device__ __forceinline__ int kv8_prompt_swizzle(int token)
     else return ((token >> 2) & 1) | ((token >> 2) & 2);
 }
 
+// v in units of 2^-8 of its row's largest element's binade, as `PIECES` E4M3 numbers, each of 2^-5 times the unit of the one before: four bits and
+// the sign of the rest each, so that two hold a bfloat16 number and three a binary16 number exactly, down to 2^-14 of the largest; below that the
+// rest is at most 2^-18 of it with one piece, 2^-23 with two, 2^-28 with three.  Four numbers to a dword of each piece.
+template <int PIECES>
+__device__ __forceinline__ void kv8_query_pieces(const float (&v)[4], int (&piece)[PIECES])
+{
+    float r[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        piece[p] = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false), true);
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(piece[p], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(piece[p], true);
+        r[0] = 32.0f * (r[0] - a[0]);
+        r[1] = 32.0f * (r[1] - a[1]);
+        r[2] = 32.0f * (r[2] - b[0]);
+        r[3] = 32.0f * (r[3] - b[1]);
+    }
+}
+
 template <int D, int QP, int PP>
 __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 {
@@ -463,7 +481,9 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
     const int token = first + min(my, n_rows - 1) / a.rep, head = hk * a.rep + min(my, n_rows - 1) % a.rep;
     const size_t out_row = static_cast<size_t>(token) * a.H_q + head;
 
-    v8h qh[KL][2], ql[QP == 2 ? KL : 1][2];
+    constexpr bool CODES = QP != 0;  // the query in E4M3 pieces, which meet the codes as they are; otherwise as pairs of binary16 numbers
+    v8h qh[CODES ? 1 : KL][2], ql[CODES ? 1 : KL][2];
+    v8i qc[CODES ? QP : 1][KL / 2];
     float unit;
     {
         float t[KL][2][8], top = 0.0f;
@@ -477,16 +497,28 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             }
         top = kv8_swap32_max(top);
         const int E = __builtin_amdgcn_frexp_expf(top);
+        constexpr int BITS = CODES ? 8 : 14;  // the largest element becomes 2^(BITS - 1) .. 2^BITS
 #pragma unroll
         for (int k = 0; k < KL; ++k)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], 14 - E);
-                qh[k][x] = kv8_round(t[k][x]);
-                if constexpr (QP == 2) ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
+                for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], BITS - E);
+                if constexpr (CODES) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        const float v[4] = {t[k][x][e], t[k][x][e + 1], t[k][x][e + 2], t[k][x][e + 3]};
+                        int piece[QP];
+                        kv8_query_pieces<QP>(v, piece);
+#pragma unroll
+                        for (int p = 0; p < QP; ++p) qc[p][k / 2][4 * (k & 1) + 2 * x + e / 4] = piece[p];
+                    }
+                } else {
+                    qh[k][x] = kv8_round(t[k][x]);
+                    ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
+                }
             }
-        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
+        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - BITS);
     }
 
     auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
@@ -548,19 +580,28 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
         for (int tb = 0; tb < 2; ++tb) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) S[tb][e] = 0.0f;
-            const int tk = 32 * tb + c;
-            const unsigned char* const at = &kt[buf][tk * D];
-            const int f = kv8_prompt_swizzle<D>(tk);
+            const unsigned char* const at = &kt[buf][(32 * tb + c) * D];
+            const int f = kv8_prompt_swizzle<D>(c);
 #pragma unroll
-            for (int k = 0; k < KL; ++k) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(at + (((2 * k + hh) ^ f) * 16));
-                const v8h k0 = kv8_halves(w[0], w[1]), k1 = kv8_halves(w[2], w[3]);
-                if constexpr (QP == 2) {
-                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[k][0], S[tb], 0, 0, 0);
-                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[k][1], S[tb], 0, 0, 0);
+            for (int k = 0; k < KL; k += 2) {
+                const u32x4 w0 = *reinterpret_cast<const u32x4*>(at + (((2 * k + hh) ^ f) * 16)), w1 = *reinterpret_cast<const u32x4*>(at + (((2 * k + 2 + hh) ^ f) * 16));
+                if constexpr (CODES) {
+                    const v8i w = {static_cast<int>(w0[0]), static_cast<int>(w0[1]), static_cast<int>(w0[2]), static_cast<int>(w0[3]),
+                                   static_cast<int>(w1[0]), static_cast<int>(w1[1]), static_cast<int>(w1[2]), static_cast<int>(w1[3])};
+#pragma unroll
+                    for (int p = QP - 1; p >= 0; --p)  // E4M3 times E4M3, the query's scale 2^(-5 p)
+                        S[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, qc[p][k / 2], S[tb], 0, 0, 0, 127, 0, 127 - 5 * p);
+                } else {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const u32x4 x = y == 0 ? w0 : w1;
+                        const v8h k0 = kv8_halves(x[0], x[1]), k1 = kv8_halves(x[2], x[3]);
+                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[k + y][0], S[tb], 0, 0, 0);
+                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[k + y][1], S[tb], 0, 0, 0);
+                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[k + y][0], S[tb], 0, 0, 0);
+                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k + y][1], S[tb], 0, 0, 0);
+                    }
                 }
-                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[k][0], S[tb], 0, 0, 0);
-                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k][1], S[tb], 0, 0, 0);
             }
         }
         float ks[4], vi[4], vl[4];
@@ -730,10 +771,12 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
             const unsigned grid = static_cast<unsigned>(plan.tiles) * static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv);
             auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
             const bool p2 = c.out_dtype == RCP_F32;
-            if (q2 && p2) launch(&kv8_prompt_kernel<D, 2, 2>);
-            else if (q2) launch(&kv8_prompt_kernel<D, 2, 1>);
-            else if (p2) launch(&kv8_prompt_kernel<D, 1, 2>);
-            else launch(&kv8_prompt_kernel<D, 1, 1>);
+            if (q2 && p2) launch(&kv8_prompt_kernel<D, 0, 2>);
+            else if (q2) launch(&kv8_prompt_kernel<D, 0, 1>);
+            else if (c.q_dtype == RCP_F16 && p2) launch(&kv8_prompt_kernel<D, 3, 2>);
+            else if (c.q_dtype == RCP_F16) launch(&kv8_prompt_kernel<D, 3, 1>);
+            else if (p2) launch(&kv8_prompt_kernel<D, 2, 2>);
+            else launch(&kv8_prompt_kernel<D, 2, 1>);
         }
     };
     if (c.D == 128) form(std::integral_constant<int, 128>{});
