@@ -592,7 +592,7 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
  * rcp_kv8_attn: row i of sequence b attends to the cached tokens of b at positions 0 .. its own:
  *     out[i][h] = sum_t softmax_t(softmax_scale * q[i][h] . K[g][t]) * V[g][t],   g = h / (H_q / H)
  *   q: [rows][H_q][D] of `q_dtype`; out: [rows][H_q][D] of `out_dtype` (any rcp_dtype).  A row that sees no token (an empty sequence, no
- *   page) gets zeros.  Tokens behind a row's own never enter, whatever bytes their slots hold; codes within a sequence must not be NaN
+ *   page) gets zeros.  softmax_scale: finite and not negative (RCP_ERR_UNSUPPORTED).  Tokens behind a row's own never enter, whatever bytes their slots hold; codes within a sequence must not be NaN
  *   (rcp_kv8_append writes none).  Sums are binary32.  The softmax weights enter the product with the values as binary16 numbers, or
  *   as pairs of them (22 bits) for binary32 results and, with one token a sequence, binary16 ones; a binary32 query as pairs, scaled by its largest element.
  *   workspace: rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, starts == NULL) bytes, overwritten by every call.  Calls that

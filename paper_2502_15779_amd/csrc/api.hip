@@ -820,6 +820,8 @@ int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const v
         return fail(RCP_ERR_SHAPE, "%s: H_q=%d must be a positive multiple of H=%d, at most 4096", fn, H_q, cache->H);
     if (!any_dtype(q_dtype) || !any_dtype(out_dtype))
         return fail(RCP_ERR_UNSUPPORTED, "%s: unknown dtype (q %d, out %d)", fn, static_cast<int>(q_dtype), static_cast<int>(out_dtype));
+    if (!(softmax_scale >= 0.0f) || softmax_scale > 3.402823466e+38f)
+        return fail(RCP_ERR_UNSUPPORTED, "%s: softmax_scale=%g must be finite and not negative", fn, static_cast<double>(softmax_scale));
     if (batch->rows == 0) return RCP_OK;
     if (!q || !out) return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);

@@ -91,8 +91,11 @@ __device__ __forceinline__ void kv8_put(void* out, int dt, size_t i, float v)
     else static_cast<__bf16*>(out)[i] = static_cast<__bf16>(v);
 }
 
-// Scales are 2^-40 .. 2^120, and a page that was never written has 0 (and zeros for codes): as a weight's factor, the nearest of those.
+// Scales are 2^-40 .. 2^120, and a page that was never written has 0 (and zeros for codes): the nearest of those stands in for it.
 constexpr float KV8_LEAST = 0x1p-40f, KV8_MOST = 0x1p120f;
+// The least factor of a score where a token is masked, by a score of -infinity: 0 (of a tiny query) would make that a NaN.  What it adds to the
+// scores of other tokens, at most 2^-126 * 2^31, is nothing.
+constexpr float KV8_NOT_ZERO = 0x1p-126f;
 
 // the page that holds position `pos` of sequence b, -1 where there is none
 __device__ __forceinline__ int kv8_page(const Kv8Table& t, const int* row, int pos)
@@ -182,7 +185,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
         const int pos = base + 16 * lane;
         page = pos < t_end ? kv8_page(a.t, a.t.table + static_cast<size_t>(b) * a.t.width, pos) : -1;
         const size_t s = static_cast<size_t>(max(page, 0)) * a.H_kv + hk;
-        k_scale = a.k_scales[s];
+        k_scale = __builtin_amdgcn_fmed3f(a.k_scales[s], KV8_LEAST, KV8_MOST);
         const float v_scale = __builtin_amdgcn_fmed3f(a.v_scales[s], KV8_LEAST, KV8_MOST);
         v_inverse = 1.0f / v_scale;
         v_log = __builtin_amdgcn_logf(v_scale);
@@ -282,6 +285,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             if (!whole) {  // uniform
+                ks[n] = fmaxf(ks[n], KV8_NOT_ZERO);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) S[n][j] = there[n] && base + 16 * n + 4 * g + j < t_end ? S[n][j] : -INFINITY;
             }
@@ -562,7 +566,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             page = look_up(tile);
             const size_t s = static_cast<size_t>(max(page, 0)) * a.H_kv + hk;
             const float v_scale = __builtin_amdgcn_fmed3f(a.v_scales[s], KV8_LEAST, KV8_MOST);
-            k_scale = a.k_scales[s];
+            k_scale = __builtin_amdgcn_fmed3f(a.k_scales[s], KV8_LEAST, KV8_MOST);
             v_inverse = 1.0f / v_scale;
             v_log = __builtin_amdgcn_logf(v_scale);
         }
@@ -621,6 +625,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
         for (int n = 0; n < 4; ++n) {
             by[n] = ks[n] * unit;
             if (!whole) {
+                by[n] = fmaxf(by[n], KV8_NOT_ZERO);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const bool seen = there[n] && base + 16 * n + 8 * (e >> 2) + 4 * hh + (e & 3) < limit;

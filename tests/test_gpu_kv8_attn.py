@@ -189,6 +189,22 @@ def test_pages_of_very_different_scales(one):
 
 
 @pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("size,scale", [(1.0, 0.1), (1.0, 0.0), (0.0, 0.1), (2.0 ** -130, 0.1), (2.0 ** -100, 2.0 ** -60), (2.0 ** 60, 2.0 ** -62)])
+def test_scores_of_nothing(one, size, scale):
+    """Pages never written (zeros with scale 0, page 0 among them), masked slots beside scores of zero or next to it, and queries of any size."""
+    D, page, H = 128, 16, 2
+    g = torch.Generator().manual_seed(12)
+    caches = _cache(g, 9, H, page, D)
+    for t in caches:
+        t[[0, 2, 4]] = torch.zeros_like(t[[0, 2, 4]])
+    q = torch.randn((3, 2 * H, D), generator=g) * size
+    lengths, starts, table = ([70, 3, 90], None, _int([[1, 2, 3, 4, 0, 5], [6, -1, -1, -1, -1, -1], [7, 8, -1, 2, 1, 3]])) if one else \
+        ([70, 3], [0, 2, 3], _int([[1, 2, 3, 4, 0], [6, -1, 5, 5, 5]]))
+    for out in (torch.float32, torch.float16):
+        _check(q, lengths, starts, table, caches, scale, out)
+
+
+@pytest.mark.parametrize("one", [True, False])
 def test_rows_are_independent(one):
     """An infinite or NaN query, or one of another magnitude, changes no other row or head."""
     D, page, H, rep = 64, 32, 2, 4

@@ -84,6 +84,8 @@ def test_attention_refusals():
     one = _batch(starts=None, rows=2)
     assert f(wb=L.rcp_kv8_workspace_bytes(2, 2, 4, 2, 64, 1) - 1, b=one) == -5
     assert f(q=None, out=None, ws=None, wb=0, b=_batch(rows=0)) == 0
+    for scale in (-0.1, float("inf"), float("nan")):
+        assert L.rcp_kv8_attn(c, _batch(), FAKE, 0, 4, scale, FAKE, 0, FAKE, 1 << 30, None) == -4 and b"softmax_scale" in L.rcp_last_error()
     w = L.rcp_kv8_workspace_bytes
     assert w(5, 0, 4, 2, 64, 0) == 0 and w(5, 2, 3, 2, 64, 0) == 0 and w(5, 2, 4, 2, 80, 0) == 0 and w(-1, 2, 4, 2, 64, 0) == 0
 
