@@ -769,7 +769,7 @@ int rcp_kv8_append(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const
         return fail(RCP_ERR_SHAPE, "%s: token strides must be multiples of 8 that hold a token's heads", fn);
     if (q_or_null && (H_q < 1 || H_q > 4096)) return fail(RCP_ERR_SHAPE, "%s: H_q=%d out of range", fn, H_q);
     const int shift = shift_of(cache->page);
-    const long long groups = 2LL * cache->H * ((batch->rows >> shift) + 2LL * batch->sequences) + 1;
+    const long long groups = 2LL * cache->H * ((batch->rows >> shift) + 2LL * batch->sequences + 8) + 1;
     if (groups + static_cast<long long>(batch->rows) * (q_or_null ? H_q : 0) > 0x7fffffffLL)
         return fail(RCP_ERR_SHAPE, "%s: %d rows of %d and %d heads are too many", fn, batch->rows, cache->H, H_q);
     if (!aligned16(k) || !aligned16(v) || !aligned16(q_or_null) || !aligned16(q_out_or_null) || !aligned16(rope_or_null))

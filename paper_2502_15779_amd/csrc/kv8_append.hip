@@ -14,6 +14,8 @@
 
 namespace rcp {
 
+constexpr int KV8_QUERIES = 4;  // query vectors of a lane in a prompt
+
 struct Kv8AppendArgs {
     Kv8Table t;
     const void *k, *v, *q;
@@ -171,26 +173,45 @@ __device__ __forceinline__ void kv8_store(void* p, size_t i, const float (&v)[8]
     }
 }
 
-// the queries of 256 / (D / 8) consecutive (token, head) rows
-template <int DT, int D>
+// The queries of U x 256 / (D / 8) consecutive (token, head) rows.  In a prompt several vectors a lane, whose loads are under way together, and the
+// starts of the sequences in LDS: a search through them in memory is a chain of loads (7273 tokens of 32 + 2 x 8 heads of 128 57 us instead of
+// 44; with eight vectors a lane 52).
+template <int DT, int D, int U>
 __device__ __forceinline__ void kv8_queries(const Kv8AppendArgs& a, int block)
 {
-    constexpr int LANES = D / 8;
-    const int row = block * (256 / LANES) + threadIdx.x / LANES, l = threadIdx.x % LANES;
-    const int t = row / a.H_q, h = row - t * a.H_q;
-    // rows beyond the call and rows of no sequence take no part; the lanes of a vector agree
-    int b = -1;
-    if (t < a.rows) b = a.t.starts == nullptr ? t : kv8_sequence_of(a.t.starts, a.t.sequences, t, a.rows);
-    int pos = -1;
-    if (b >= 0) {
-        const Kv8Run r = kv8_run(a.t.starts, a.t.lengths, b, a.rows);
-        pos = r.pos + (t - r.first);
+    constexpr int LANES = D / 8, ROWS = 256 / LANES;
+    __shared__ int starts[U == 1 ? 1 : KV8_MOST_SEQUENCES + 1];
+    const int l = threadIdx.x % LANES;
+    if constexpr (U > 1) {
+        for (int i = threadIdx.x; i <= a.t.sequences; i += 256) starts[i] = a.t.starts[i];
+        __syncthreads();
     }
-    if (pos < 0 || pos >= a.t.capacity) return;
-    float v[8];
-    load8_as_float<DT>(a.q, static_cast<size_t>(t) * a.q_stride + h * D + 8 * l, v);
-    kv8_turn<D>(v, l, a.rope != nullptr ? a.rope + static_cast<size_t>(pos) * D : nullptr, a.rotate != 0);
-    kv8_store<DT>(a.q_out, (static_cast<size_t>(t) * a.H_q + h) * D + 8 * l, v);
+    Raw8<DT> raw[U];
+    int pos[U];
+    size_t to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int row = (block * U + u) * ROWS + threadIdx.x / LANES;
+        const int t = row / a.H_q, h = row - t * a.H_q;
+        // rows beyond the call and rows of no sequence take no part; the lanes of a vector agree
+        int b = -1;
+        if (t < a.rows) b = U == 1 ? t : kv8_sequence_of(starts, a.t.sequences, t, a.rows);
+        pos[u] = -1;
+        if (b >= 0) {
+            raw[u] = load8_raw<DT>(a.q, static_cast<size_t>(t) * a.q_stride + h * D + 8 * l);
+            const Kv8Run r = kv8_run(U == 1 ? nullptr : starts, a.t.lengths, b, a.rows);
+            pos[u] = r.pos + (t - r.first);
+        }
+        to[u] = (static_cast<size_t>(t) * a.H_q + h) * D + 8 * l;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (pos[u] < 0 || pos[u] >= a.t.capacity) continue;
+        float v[8];
+        widen8<DT>(raw[u], v);
+        kv8_turn<D>(v, l, a.rope != nullptr ? a.rope + static_cast<size_t>(pos[u]) * D : nullptr, a.rotate != 0);
+        kv8_store<DT>(a.q_out, to[u], v);
+    }
 }
 
 // One new token a sequence: a vector is all that its page and head gets, so that its lanes need no other wavefront.
@@ -199,7 +220,7 @@ __global__ __launch_bounds__(256) void kv8_append_one_kernel(Kv8AppendArgs a)
 {
     constexpr int LANES = D / 8, ROWS = 256 / LANES;
     if (static_cast<int>(blockIdx.x) >= a.kv_groups) {
-        kv8_queries<DT, D>(a, blockIdx.x - a.kv_groups);
+        kv8_queries<DT, D, 1>(a, blockIdx.x - a.kv_groups);
         return;
     }
     const int half = a.kv_groups / 2;
@@ -242,10 +263,13 @@ __global__ __launch_bounds__(256) void kv8_append_pages_kernel(Kv8AppendArgs a)
     constexpr int LANES = D / 8, ROWS = 256 / LANES;
     __shared__ uint32_t red[4];
     if (static_cast<int>(blockIdx.x) >= a.kv_groups) {
-        kv8_queries<DT, D>(a, blockIdx.x - a.kv_groups);
+        kv8_queries<DT, D, KV8_QUERIES>(a, blockIdx.x - a.kv_groups);
         return;
     }
-    const int unit_of = static_cast<int>(blockIdx.x) / (2 * a.H), part = static_cast<int>(blockIdx.x) - unit_of * 2 * a.H;
+    // Workgroups go to the eight dies in turn; a die gets all heads of a page one after the other, since they read the same angles (7273 tokens
+    // of 32 + 2 x 8 heads of 128 42.4 us, with a die to each head 44.5; without a position rotation 36.9 and 36.4).
+    const int eighth = static_cast<int>(blockIdx.x) >> 3, round = eighth / (2 * a.H), part = eighth - round * 2 * a.H;
+    const int unit_of = 8 * round + (static_cast<int>(blockIdx.x) & 7);
     const bool values = part >= a.H;
     const int h = values ? part - a.H : part;
     const int tid = threadIdx.x, lane = tid & 63, l = tid % LANES;
@@ -325,8 +349,9 @@ int launch_kv8_append(const Kv8AppendCall& c, hipStream_t st)
     const int vectors = 2048 / c.D;  // of a workgroup
     const bool one = c.starts == nullptr;
     a.kv_groups = one ? 2 * ((c.sequences * c.H + vectors - 1) / vectors)
-                      : static_cast<int>(kv8_most_pages(c.rows, c.sequences, c.shift)) * 2 * c.H;
-    const long long q_groups = (static_cast<long long>(c.rows) * a.H_q + vectors - 1) / vectors;
+                      : static_cast<int>((kv8_most_pages(c.rows, c.sequences, c.shift) + 7) / 8 * 8) * 2 * c.H;
+    const int q_vectors = one ? vectors : KV8_QUERIES * vectors;
+    const long long q_groups = (static_cast<long long>(c.rows) * a.H_q + q_vectors - 1) / q_vectors;
     const unsigned grid = static_cast<unsigned>(a.kv_groups + q_groups);
     auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
     const int passes = (c.D << c.shift) / 2048;  // vectors a lane for a whole page: 0 (half a pass), 1, 2, 4, 8
