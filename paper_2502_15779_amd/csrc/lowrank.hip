@@ -138,10 +138,11 @@ __global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
     }
 }
 
-// Many tokens: workgroup = (split of K, slot of leaders, 64 tokens), sixteen tokens of each wavefront.  x and A come through LDS in stages of 128 columns, two
-// of them, so that a load takes 256 bytes of a row: read in the products' own order, 64 bytes of each of sixteen rows whose distance is a multiple of
-// 4 KB meet in one channel of the cache (2001 tokens, K = 14336: 27 us).  Piece p (16 bytes) of row n stands at place p ^ (n % 16).
-constexpr int LOWRANK_STAGE = 128;
+// Many tokens: workgroup = (split of K, slot of leaders, 64 tokens), sixteen tokens of each wavefront.  Bound by the memory x comes from (2001 tokens, K = 14336,
+// r = 64, bfloat16: 57 MB in 18.8 us, 3.1 TB/s).  x and A come through LDS in stages of 64 columns, so that the four wavefronts share A and a load takes 128 bytes
+// of a row; three stages, so that two are under way (two stages: as fast there).  Piece p (16 bytes) of row n stands at place p ^ (n / 2 % 8): the sixteen
+// rows that are read together, 128 bytes each, fall into different banks.
+constexpr int LOWRANK_STAGE = 64, LOWRANK_STAGES = 3;
 
 __device__ __forceinline__ void lowrank_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* to, int offset)
 {
@@ -152,10 +153,10 @@ template <int DT, int NR>
 __global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
 {
     constexpr int ROW = LOWRANK_STAGE * 2;  // bytes
-    __shared__ __attribute__((aligned(16))) unsigned char xs[2][64 * ROW], as[2][16 * NR * ROW];
+    __shared__ __attribute__((aligned(16))) unsigned char xs[LOWRANK_STAGES][64 * ROW], as[LOWRANK_STAGES][16 * NR * ROW];
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = static_cast<int>(blockIdx.z) * 64;
+    const int m0 = static_cast<int>(blockIdx.y) * 64;
     const int id = lowrank_adapter(a, m0 + lane);
     int order;
     unsigned long long leaders = lowrank_leaders(id, 64, order);
@@ -166,42 +167,50 @@ __global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
     };
     const __amdgpu_buffer_rsrc_t xr = resource(a.x, m0, min(64, a.M - m0), a.K);
     for (int slot = 0; leaders != 0; ++slot, leaders &= leaders - 1) {
-        if (slot % a.slots != static_cast<int>(blockIdx.y)) continue;  // uniform
+        if (slot % a.slots != static_cast<int>(blockIdx.z)) continue;  // uniform
         const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
         for (int r0 = 0; r0 < a.r; r0 += 16 * NR) {
             const int ranks = min(16 * NR, a.r - r0);
             const __amdgpu_buffer_rsrc_t ar = resource(a.A, static_cast<size_t>(adapter) * a.r + r0, ranks, a.K);  // ranks beyond the last read zeros
-            auto stage = [&](int k, int buf) {  // four rows a load
-                const int piece = lane & 15;
+            constexpr int X_LOADS = 2, A_LOADS = NR == 1 ? 1 : NR / 2;
+            auto stage = [&](int k, int buf) {  // eight rows a load; beyond the last column: zeros that nobody takes, but as many loads
+                const int piece = lane & 7, beyond = k < k1 ? 0 : 1 << 30;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int row = 16 * wave + 4 * y + (lane >> 4);
-                    lowrank_to_lds(xr, &xs[buf][(16 * wave + 4 * y) * ROW], (row * a.K + k) * 2 + 16 * (piece ^ (row & 15)));
+                for (int y = 0; y < X_LOADS; ++y) {
+                    const int row = 16 * wave + 8 * y + (lane >> 3);
+                    lowrank_to_lds(xr, &xs[buf][(16 * wave + 8 * y) * ROW], ((row * a.K + k) * 2 + 16 * (piece ^ (row >> 1 & 7))) | beyond);
                 }
 #pragma unroll
-                for (int y = 0; y < NR; ++y) {
-                    const int row = 4 * NR * wave + 4 * y + (lane >> 4);
-                    lowrank_to_lds(ar, &as[buf][(4 * NR * wave + 4 * y) * ROW], (row * a.K + k) * 2 + 16 * (piece ^ (row & 15)));
+                for (int y = 0; y < A_LOADS; ++y) {  // (sixteen ranks: two wavefronts each load the same eight)
+                    const int first = NR == 1 ? 8 * (wave & 1) : 4 * NR * wave + 8 * y, row = first + (lane >> 3);
+                    lowrank_to_lds(ar, &as[buf][first * ROW], ((row * a.K + k) * 2 + 16 * (piece ^ (row >> 1 & 7))) | beyond);
                 }
             };
             v4f acc[NR];
 #pragma unroll
             for (int n = 0; n < NR; ++n) acc[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            stage(k0, 0);
-            for (int k = k0, buf = 0; k < k1; k += LOWRANK_STAGE, buf ^= 1) {
-                __builtin_amdgcn_s_waitcnt(0);  // this wavefront's part of the stage is in LDS,
-                __syncthreads();                // everybody's is, and the other buffer has been read
-                if (k + LOWRANK_STAGE < k1) stage(k + LOWRANK_STAGE, buf ^ 1);
+#pragma unroll
+            for (int x = 0; x < LOWRANK_STAGES - 1; ++x) stage(k0 + LOWRANK_STAGE * x, x);
+            for (int k = k0, buf = 0; k < k1; k += LOWRANK_STAGE) {
+                // this wavefront's part of the stage is in LDS once only the later ones' loads are outstanding,
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(((X_LOADS + A_LOADS) * (LOWRANK_STAGES - 2)) | (7 << 4) | (15 << 8));
+                __syncthreads();  // then everybody's is, and the stage before has been read
+                __builtin_amdgcn_sched_barrier(0);
+                stage(k + LOWRANK_STAGE * (LOWRANK_STAGES - 1), buf == 0 ? LOWRANK_STAGES - 1 : buf - 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int s = 0; s < LOWRANK_STAGE / LOWRANK_STEP; ++s) {
                     if (k + LOWRANK_STEP * s >= k1) break;  // uniform
-                    const int at = ((4 * s + g) ^ i) * 16;
+                    const int at = ((4 * s + g) ^ (i >> 1)) * 16;
                     const Eight<DT> xv = *reinterpret_cast<const Eight<DT>*>(&xs[buf][(16 * wave + i) * ROW + at]);
 #pragma unroll
                     for (int n = 0; n < NR; ++n)
                         acc[n] = lowrank_mfma<DT>(*reinterpret_cast<const Eight<DT>*>(&as[buf][(16 * n + i) * ROW + at]), xv, acc[n]);
                 }
+                buf = buf == LOWRANK_STAGES - 1 ? 0 : buf + 1;
             }
+            __builtin_amdgcn_s_waitcnt(0);  // nothing is on its way into LDS any more
             if (mine == adapter) {
                 float* const to = a.part + (static_cast<size_t>(blockIdx.x) * a.M + m0 + 16 * wave + i) * a.r;
 #pragma unroll
@@ -520,7 +529,10 @@ int launch_lowrank(const void* x, rcp_dtype dt, int M, int N, int K, int r, int 
 {
     const LowrankPlan p = lowrank_plan(M, K);
     LowrankArgs a = {x, A, B, base, which, scaling, out, static_cast<float*>(workspace), M, N, K, r, adapters, p.splits, p.chunk, p.slots};
-    const dim3 grid(static_cast<unsigned>(p.splits), static_cast<unsigned>(p.slots), static_cast<unsigned>(p.tiles));
+    // Many tokens: most tiles have one adapter, so the slots behind the first come last; among the others, their workgroups, which end at once, would leave
+    // a part of the compute units without work (2001 tokens, K = 14336, r = 64: 27 us instead of 18.8).
+    const unsigned slots = static_cast<unsigned>(p.slots), tiles_in = static_cast<unsigned>(p.tiles);
+    const dim3 grid(static_cast<unsigned>(p.splits), p.many ? tiles_in : slots, p.many ? slots : tiles_in);
     const unsigned tiles = static_cast<unsigned>((M + 15) / 16);
     // Many tokens: workgroups go to the eight dies, each with a cache of its own, in turn; with a width of whole eights those that add up the same partial
     // sums meet on one die.
