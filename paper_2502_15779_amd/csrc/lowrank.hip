@@ -72,14 +72,14 @@ __global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
     __shared__ float red[3][NR][256];
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int m0 = static_cast<int>(blockIdx.z) * 16;
+    const int m0 = static_cast<int>(blockIdx.y) * 16;
     const int id = lane < 16 ? lowrank_adapter(a, m0 + lane) : -1;
     int order;
     unsigned long long leaders = lowrank_leaders(id, 16, order);
     const int quarter = a.chunk / 4, k0 = static_cast<int>(blockIdx.x) * a.chunk + quarter * wave, k1 = min(a.K, k0 + quarter);
     const auto* const x = static_cast<const One<DT>*>(a.x) + static_cast<size_t>(min(m0 + i, a.M - 1)) * a.K + 8 * g;  // beyond the last token: that again
     for (int slot = 0; leaders != 0; ++slot, leaders &= leaders - 1) {
-        if (slot % a.slots != static_cast<int>(blockIdx.y)) continue;  // uniform
+        if (slot % a.slots != static_cast<int>(blockIdx.z)) continue;  // uniform
         const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
         const auto* const A = static_cast<const One<DT>*>(a.A) + static_cast<size_t>(adapter) * a.r * a.K + 8 * g;
         for (int r0 = 0; r0 < a.r; r0 += 16 * NR) {
@@ -529,10 +529,9 @@ int launch_lowrank(const void* x, rcp_dtype dt, int M, int N, int K, int r, int 
 {
     const LowrankPlan p = lowrank_plan(M, K);
     LowrankArgs a = {x, A, B, base, which, scaling, out, static_cast<float*>(workspace), M, N, K, r, adapters, p.splits, p.chunk, p.slots};
-    // Many tokens: most tiles have one adapter, so the slots behind the first come last; among the others, their workgroups, which end at once, would leave
-    // a part of the compute units without work (2001 tokens, K = 14336, r = 64: 27 us instead of 18.8).
-    const unsigned slots = static_cast<unsigned>(p.slots), tiles_in = static_cast<unsigned>(p.tiles);
-    const dim3 grid(static_cast<unsigned>(p.splits), p.many ? tiles_in : slots, p.many ? slots : tiles_in);
+    // Most tiles have one adapter, so the slots behind the first come last; among the others, their workgroups, which end at once, would leave a part of the
+    // compute units without work (2001 tokens, K = 14336, r = 64: 27 us instead of 18.8).
+    const dim3 grid(static_cast<unsigned>(p.splits), static_cast<unsigned>(p.tiles), static_cast<unsigned>(p.slots));
     const unsigned tiles = static_cast<unsigned>((M + 15) / 16);
     // Many tokens: workgroups go to the eight dies, each with a cache of its own, in turn; with a width of whole eights those that add up the same partial
     // sums meet on one die.
