@@ -725,11 +725,11 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
     }
 }
 
-// blockIdx = (query head, row of the call)
+// blockIdx = the query heads of a row of the call, row after row
 template <int D, int GROUPS>
 __global__ __launch_bounds__(GROUPS * D) void kv8_prompt_merge_kernel(Kv8AttnArgs a)
 {
-    const int h = blockIdx.x, t = blockIdx.y;
+    const int t = static_cast<int>(blockIdx.x) / a.H_q, h = static_cast<int>(blockIdx.x) - t * a.H_q;
     if (kv8_sequence_of(a.t.starts, a.t.sequences, t, a.rows) < 0) return;
     const size_t row = static_cast<size_t>(t) * a.H_q + h, stride = static_cast<size_t>(a.rows) * a.H_q * (D + KV8_EXTRA);
     kv8_merge<D, GROUPS>(a.part + row * (D + KV8_EXTRA), stride, a.chunks, a.out, a.out_dt, row);
@@ -822,7 +822,8 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
     else form(std::integral_constant<int, 64>{});
     if (int rc = check_launch("rcp_kv8_attn")) return rc;
     if (!one && plan.chunks == 1) return RCP_OK;
-    const dim3 grid(static_cast<unsigned>(c.H_q), static_cast<unsigned>(one ? c.sequences : c.rows));
+    // (a second dimension ends at 65535; rows are split only where there are few of them, times query heads)
+    const dim3 grid = one ? dim3(static_cast<unsigned>(c.H_q), static_cast<unsigned>(c.sequences)) : dim3(static_cast<unsigned>(c.H_q) * static_cast<unsigned>(c.rows));
     // wavefronts for the partial results of a row: eight to a thread at a time
     auto merge = [&](auto size) {
         constexpr int D = decltype(size)::value;

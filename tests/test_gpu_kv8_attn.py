@@ -244,6 +244,15 @@ def test_a_token_behind_a_row_never_enters():
     assert torch.equal(a[:48], b[:48]) and not torch.equal(a[48:], b[48:])
 
 
+@pytest.mark.parametrize("first", [0, 69997])
+def test_a_few_rows_of_a_wide_padded_call(first):
+    """More rows than a grid's second dimension holds, three of which belong to a sequence."""
+    g = torch.Generator().manual_seed(13)
+    caches = _cache(g, 12, 1, 64, 64)
+    q = torch.randn((70000, 1, 64), generator=g).half()
+    _check(q, [700], [first, first + 3], torch.arange(12).int()[None], caches, 0.125, torch.float16)
+
+
 def test_outputs_made_here_and_workspaces_given():
     D, H = 64, 2
     g = torch.Generator().manual_seed(7)
