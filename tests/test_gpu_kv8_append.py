@@ -98,6 +98,19 @@ def test_ragged_runs(D, page, dtype, H, rotate):
     _check(x[:, 2 * H:3 * H], x[:, 3 * H:], lengths, starts, table, caches, ref.rope_table(table.shape[1] * page, D), rotate, x[:, :2 * H])
 
 
+def test_more_sequences_than_lanes():
+    D, page, H = 64, 16, 2
+    new = [(b * 7) % 4 for b in range(140)]
+    lengths, starts = [n + (b * 5) % 40 for b, n in enumerate(new)], [1]
+    for x in new:
+        starts.append(starts[-1] + x)
+    g, _ = _state(16, 1, 1, 16, 64)
+    table, n = _tables(g, lengths, page)
+    _, caches = _state(17, n, H, page, D)
+    k, v = (torch.randn((starts[-1] + 2, H, D), generator=g).half() for _ in range(2))
+    _check(k, v, lengths, starts, table, caches, ref.rope_table(table.shape[1] * page, D), True, torch.randn((starts[-1] + 2, 3, D), generator=g).half())
+
+
 def test_scales_grow_and_pages_start_anew():
     """Token after token with magnitudes that rise and fall: the scale only grows within a page, older codes are rounded to it, and the next page's first token
     ignores what the page held (a scale of 2^30)."""
@@ -226,3 +239,24 @@ def test_a_capture_follows_lengths_and_tables():
         rows = [b for b in range(2) if n[b] > 0]
         assert torch.equal(replayed[rows], q_out[rows])
         assert all(torch.equal(a.float(), b.float()) for a, b in zip(dev, other))
+
+
+@pytest.mark.parametrize("change, message", [
+    (dict(rope=(47, 64)), "rope must be"), (dict(rope=(48, 32)), "rope must be"), (dict(rope=(48, 64), rope_dtype=torch.float64), "rope must be"),
+    (dict(q=(2, 4, 32)), "q"), (dict(q=(3, 4, 64)), "q must be"), (dict(q=(2, 4, 64), q_dtype=torch.bfloat16), "q must be"),
+    (dict(q=(2, 4, 64), q_out=(2, 3, 64)), "q_out must be"), (dict(q_out=(2, 4, 64)), "q_out without q"), (dict(k=(2, 2, 32)), "k"), (dict(k=(1, 2, 64)), "as many tokens"),
+    (dict(wide=8 + 2), "multiple"), (dict(lengths=(3,)), "lengths"), (dict(table=(1, 3)), "table")])
+def test_refusals(change, message):
+    caches = [t.to(DEV) for t in _state(15, 6, 2, 16, 64)[1]]
+    before = [t.clone() for t in caches]
+    made = lambda name, shape, dtype=torch.float16: torch.zeros(change.get(name, shape), dtype=change.get(name + "_dtype", dtype), device=DEV)
+    k = made("k", (2, 2, 64))
+    if "wide" in change:   # a token stride that is no multiple of 8
+        k = torch.zeros((2, 2 * 64 + change["wide"]), dtype=torch.float16, device=DEV)[:, :128].unflatten(1, (2, 64))
+    more = {name: made(name, None) for name in ("q", "q_out") if name in change}
+    if "rope" in change:
+        more["rope"] = made("rope", None, torch.float32)
+    with pytest.raises((ValueError, RuntimeError), match=message):
+        rcp.kv8_append(k, torch.zeros((2, 2, 64), dtype=torch.float16, device=DEV), made("lengths", (2,), torch.int32), made("table", (2, 3), torch.int32), *caches, **more)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(caches, before))

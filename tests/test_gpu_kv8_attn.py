@@ -142,6 +142,41 @@ def test_rows_that_fill_the_device_and_a_few_behind_a_long_context(H, rep, n, le
             assert bool(((out[i:i + 1, h * rep:h * rep + rep] - exact).abs() <= tol).all()), (h, i)
 
 
+@pytest.mark.parametrize("D,dtype,out", [(128, "bf16", "bf16"), (128, "f16", "f32"), (128, "f32", "f16"), (64, "f16", "f16"), (64, "bf16", "f32")])
+def test_ragged_rows_of_many_heads(D, dtype, out):
+    """No row is split, tiles of rows end anywhere, rows of no sequence between them stay as they are.  All heads hold the same, so all results are those of one."""
+    page, H, rep = 32, 128, 3
+    g = torch.Generator().manual_seed(D)
+    new, lengths, starts = [43, 0, 1, 90, 129], [43, 5, 60, 150, 129], [2]
+    for x in new:
+        starts.append(starts[-1] + x)
+    table = _table(g, lengths, page, 40)
+    caches = _hide(_cache(g, 40, 1, page, D), table, lengths)
+    q = torch.randn((starts[-1] + 4, rep, D), generator=g).to(DTYPES[dtype])
+    out_dtype, scale = DTYPES[out], D ** -0.5
+    got = torch.full((q.shape[0], H * rep, D), 5.0, dtype=out_dtype, device=DEV)
+    rcp.kv8_attn(q.repeat(1, H, 1).to(DEV), _int(lengths).to(DEV), table.to(DEV), *[t.repeat_interleave(H, 1).contiguous().to(DEV) for t in caches], scale,
+                 starts=_int(starts).to(DEV), out=got)
+    got = got.cpu().view(q.shape[0], H, rep, D)
+    assert torch.equal(got, got[:, :1].expand_as(got))
+    exact, mag, size, seen = ref.attention(q, lengths, starts, table, *caches, scale)
+    nobody, got = exact.isnan(), got[:, 0].double()
+    assert bool((got[nobody] == 5.0).all()) and bool(nobody[:2].all()) and bool(nobody[-4:].all()) and not bool(nobody[2:-4].any())
+    assert bool(((got - exact).abs() <= _tolerance(exact, mag, size, seen, q, out_dtype, False))[~nobody].all())
+
+
+def test_more_sequences_than_lanes():
+    D, page = 64, 16
+    g = torch.Generator().manual_seed(14)
+    new = [(b * 7) % 4 for b in range(140)]
+    lengths, starts = [n + (b * 5) % 40 for b, n in enumerate(new)], [0]
+    for x in new:
+        starts.append(starts[-1] + x)
+    table = _table(g, lengths, page, 500)
+    caches = _hide(_cache(g, 500, 1, page, D), table, lengths)
+    _check(torch.randn((starts[-1], 2, D), generator=g).half(), lengths, starts, table, caches, 0.125, torch.float32)
+
+
 @pytest.mark.parametrize("one", [True, False])
 def test_entries_that_are_no_page(one):
     """Their tokens are not attended to; a row without any token gets zeros."""
