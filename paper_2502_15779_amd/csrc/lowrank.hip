@@ -224,18 +224,6 @@ __global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
     }
 }
 
-template <int DT>
-__device__ __forceinline__ Eight<DT> lowrank_round(float (&v)[8])  // and leaves what that misses
-{
-    Eight<DT> h;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[e] = static_cast<One<DT>>(v[e]);
-        v[e] -= static_cast<float>(h[e]);
-    }
-    return h;
-}
-
 // four results of a row from index i on
 template <int DT>
 __device__ __forceinline__ void lowrank_store4(void* p, size_t i, const float* v)
@@ -273,67 +261,77 @@ __device__ __forceinline__ void lowrank_add4(const Raw4<DT>& x, float* v)
     }
 }
 
-// scaling t of a tile of sixteen tokens, summed over the splits, into LDS [16][PADDED + 4] (zeros for ranks beyond the last and tokens without an adapter)
-template <int PADDED>
-__device__ __forceinline__ void lowrank_total(const LowrankArgs& a, int m0, int id, float* sums)
+// scaling t of a tile of sixteen tokens in LDS, as the operands' pieces, and E of the binary16 scale: a token's largest value becomes 2^13 .. 2^14
+template <int DT, int STEPS>
+struct LowrankTerms {
+    static constexpr int PIECES = DT == RCP_F16 ? 2 : 3;
+    One<DT> piece[PIECES][16][32 * STEPS + 8];
+    int E[16];
+};
+
+// Sums the splits (zeros for ranks beyond the last and tokens without an adapter): sixteen lanes a token, neighbouring ranks a lane, so that the loads of eight splits
+// are eight instructions, under way together, and no value is converted twice in the workgroup.
+template <int DT, int STEPS>
+__device__ __forceinline__ void lowrank_total(const LowrankArgs& a, int m0, int id, LowrankTerms<DT, STEPS>& to)
 {
-    constexpr int MINE = 16 * PADDED / 256;  // values of a thread
-    float t[MINE], scale[MINE];
-    const float* from[MINE];
-#pragma unroll
-    for (int x = 0; x < MINE; ++x) {  // what no token has is read, too (it lies in the workspace), and dropped: no branches between the loads
-        const int at = threadIdx.x + 256 * x, token = at / PADDED, rank = at % PADDED;
-        scale[x] = a.scaling[max(__shfl(id, token, 64), 0)];
-        from[x] = a.part + static_cast<size_t>(min(m0 + token, a.M - 1)) * a.r + min(rank, a.r - 1);
-        t[x] = 0.0f;
-    }
+    constexpr int V = 2 * STEPS, U = 8;
+    typedef float Part __attribute__((ext_vector_type(V), aligned(V == 2 ? 8 : 16)));
+    typedef One<DT> Piece __attribute__((ext_vector_type(V)));
+    const int token = static_cast<int>(threadIdx.x) / 16, rank = static_cast<int>(threadIdx.x) % 16 * V;
+    const int mine = __shfl(id, token, 64);
+    const float scale = a.scaling[max(mine, 0)];
+    // what no token has is read, too (it lies in the workspace), and dropped: no branches between the loads
+    const float* const from = a.part + static_cast<size_t>(min(m0 + token, a.M - 1)) * a.r + min(rank, a.r - V);
     const size_t next = static_cast<size_t>(a.M) * a.r;
-    int k = 0;
-    for (; k + 4 <= a.splits; k += 4)
+    Part t = {};
+    for (int k = 0; k < a.splits; k += U) {
+        Part x[U];
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int y = 0; y < U; ++y) x[y] = *reinterpret_cast<const Part*>(from + min(k + y, a.splits - 1) * next);
 #pragma unroll
-            for (int x = 0; x < MINE; ++x) t[x] += from[x][(k + y) * next];
-    for (; k < a.splits; ++k)
+        for (int y = 0; y < U; ++y)
+            if (k + y < a.splits) t += x[y];  // uniform
+    }
 #pragma unroll
-        for (int x = 0; x < MINE; ++x) t[x] += from[x][k * next];
+    for (int e = 0; e < V; ++e) t[e] = mine >= 0 && rank < a.r ? t[e] * scale : 0.0f;
+    if constexpr (DT == RCP_F16) {
+        float top = 0.0f;
 #pragma unroll
-    for (int x = 0; x < MINE; ++x) {
-        const int at = threadIdx.x + 256 * x, token = at / PADDED, rank = at % PADDED;
-        sums[token * (PADDED + 4) + rank] = __shfl(id, token, 64) >= 0 && rank < a.r ? t[x] * scale[x] : 0.0f;
+        for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(t[e]));
+        auto turned = [](float v, auto by) {  // of the lane so many further in the row of sixteen
+            return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + decltype(by)::value, 0xf, 0xf, true));
+        };
+        top = fmaxf(top, turned(top, std::integral_constant<int, 8>{}));
+        top = fmaxf(top, turned(top, std::integral_constant<int, 4>{}));
+        top = fmaxf(top, turned(top, std::integral_constant<int, 2>{}));
+        top = fmaxf(top, turned(top, std::integral_constant<int, 1>{}));
+        const int E = __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[e] = ldexpf(t[e], 14 - E);
+        if (rank == 0) to.E[token] = E;
+    }
+#pragma unroll
+    for (int q = 0; q < LowrankTerms<DT, STEPS>::PIECES; ++q) {
+        Piece h;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            h[e] = static_cast<One<DT>>(t[e]);
+            t[e] -= static_cast<float>(h[e]);
+        }
+        *reinterpret_cast<Piece*>(&to.piece[q][token][rank]) = h;
     }
 }
 
-// the t of token lane % 16 as operands; returns E of the binary16 scale: its largest value becomes 2^13 .. 2^14
+// the t of token lane % 16 as operands; returns E
 template <int DT, int STEPS, int PIECES>
-__device__ __forceinline__ int lowrank_pieces(const float* sums, Eight<DT> (&piece)[STEPS][PIECES])
+__device__ __forceinline__ int lowrank_pieces(const LowrankTerms<DT, STEPS>& from, Eight<DT> (&piece)[STEPS][PIECES])
 {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-    float t[STEPS][8], top = 0.0f;
-    int E = 14;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            t[s][e] = sums[i * (32 * STEPS + 4) + 32 * s + 8 * g + e];
-            top = fmaxf(top, fabsf(t[s][e]));
-        }
-    if constexpr (DT == RCP_F16) {
-        auto swap = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
-        swap = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(swap[0]), __uint_as_float(swap[1]));
-        E = __builtin_amdgcn_frexp_expf(top);
-    }
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-        if constexpr (DT == RCP_F16)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t[s][e] = ldexpf(t[s][e], 14 - E);
-#pragma unroll
-        for (int q = 0; q < PIECES; ++q) piece[s][q] = lowrank_round<DT>(t[s]);
-    }
-    return E;
+        for (int q = 0; q < PIECES; ++q) piece[s][q] = *reinterpret_cast<const Eight<DT>*>(&from.piece[q][i][32 * s + 8 * g]);
+    return DT == RCP_F16 ? from.E[i] : 14;
 }
 
 // rows of B (ranks 32 s + 8 g ..) times t; ranks beyond the last are zeros on both sides
@@ -357,7 +355,7 @@ template <int DT, int OUT, int STEPS>
 __global__ __launch_bounds__(256) void lowrank_few_out_kernel(LowrankArgs a)
 {
     constexpr int PIECES = DT == RCP_F16 ? 2 : 3, TOGETHER = 4 / STEPS;  // adapters whose rows of B are under way at a time
-    __shared__ float sums[16 * (32 * STEPS + 4)];
+    __shared__ __attribute__((aligned(16))) LowrankTerms<DT, STEPS> terms;
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const int m0 = static_cast<int>(blockIdx.y) * 16, n0 = static_cast<int>(blockIdx.x) * 32;
@@ -392,10 +390,10 @@ __global__ __launch_bounds__(256) void lowrank_few_out_kernel(LowrankArgs a)
 #pragma unroll
     for (int p = 0; p < 2; ++p)
         if (writes && n0 + 16 * p + 4 * g < a.N) base[p] = lowrank_load4<OUT>(a.base, to + 16 * p);
-    lowrank_total<32 * STEPS>(a, m0, id, sums);
+    lowrank_total<DT, STEPS>(a, m0, id, terms);
     __syncthreads();
     Eight<DT> piece[STEPS][PIECES];
-    const int E = lowrank_pieces<DT, STEPS, PIECES>(sums, piece);
+    const int E = lowrank_pieces<DT, STEPS, PIECES>(terms, piece);
     v4f total[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
     for (;;) {
 #pragma unroll
@@ -432,6 +430,8 @@ __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
 {
     constexpr int PIECES = DT == RCP_F16 ? 2 : 3, ROW = LOWRANK_COLUMNS + 4;
     __shared__ __attribute__((aligned(16))) float block[16 * ROW];  // the products; before them, t
+    auto& terms = *reinterpret_cast<LowrankTerms<DT, STEPS>*>(block);
+    static_assert(sizeof(terms) <= sizeof(block), "t lies where the products come");
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const int m0 = static_cast<int>(blockIdx.x) * 16, n0 = static_cast<int>(blockIdx.y) * LOWRANK_COLUMNS;
@@ -451,9 +451,9 @@ __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
     Eight<DT> piece[STEPS][PIECES];
     int E = 14;
     if (leaders != 0) {  // uniform over the workgroup
-        lowrank_total<32 * STEPS>(a, m0, id, block);
+        lowrank_total<DT, STEPS>(a, m0, id, terms);
         __syncthreads();
-        E = lowrank_pieces<DT, STEPS, PIECES>(block, piece);
+        E = lowrank_pieces<DT, STEPS, PIECES>(terms, piece);
         __syncthreads();
     }
     for (; leaders != 0; leaders &= leaders - 1) {
