@@ -422,16 +422,20 @@ __global__ __launch_bounds__(256) void lowrank_few_out_kernel(LowrankArgs a)
 }
 
 // Many tokens: workgroup = (512 outputs, sixteen tokens), 128 outputs of each wavefront.  The products pass through LDS, so that base and out are read and
-// written in kilobytes of a row: in the products' own order (32 bytes of each of sixteen rows) 2001 tokens of 4096 outputs took 30 us.
+// written in kilobytes of a row: in the products' own order (32 bytes of each of sixteen rows) 2001 tokens of 4096 outputs took 30 us.  So does B of more than 32
+// ranks before them: a cache serves what neighbouring lanes read together, and in the products' order those are different rows (2001 tokens, rank 64: 25 us
+// instead of 22; but 300 tokens, tiles of sixteen adapters each, 81 us instead of 86: a wait for each of them).
+// Piece p (16 bytes) of row n of B stands at place p ^ (n / (16 / P) % P) of the P = r / 8 of its row, so that sixteen rows fall into different banks; where P is no
+// power of two, in order.
 constexpr int LOWRANK_COLUMNS = 512;
 
 template <int DT, int OUT, int STEPS>
 __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
 {
-    constexpr int PIECES = DT == RCP_F16 ? 2 : 3, ROW = LOWRANK_COLUMNS + 4;
-    __shared__ __attribute__((aligned(16))) float block[16 * ROW];  // the products; before them, t
-    auto& terms = *reinterpret_cast<LowrankTerms<DT, STEPS>*>(block);
-    static_assert(sizeof(terms) <= sizeof(block), "t lies where the products come");
+    constexpr int PIECES = DT == RCP_F16 ? 2 : 3, ROW = 128 + 4, AT_ONCE = 8 / STEPS;  // products whose rows of B are in LDS at a time: 8 KB and less
+    __shared__ __attribute__((aligned(16))) float block[4][16 * ROW];  // of each wavefront: its rows of B, then its products; before them, t
+    auto& terms = *reinterpret_cast<LowrankTerms<DT, STEPS>*>(&block[0][0]);
+    static_assert(sizeof(terms) <= sizeof(block) && sizeof(block[0]) >= 8192, "t and B lie where the products come");
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const int m0 = static_cast<int>(blockIdx.x) * 16, n0 = static_cast<int>(blockIdx.y) * LOWRANK_COLUMNS;
@@ -440,14 +444,6 @@ __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
     int order;
     unsigned long long leaders = lowrank_leaders(id, 16, order);
     const int mine = __shfl(id, i, 64);
-    // rows wave, wave + 4, ... of the tile, eight outputs a lane
-    Raw4<OUT> base[4][2];
-    const int n = n0 + 8 * lane;
-#pragma unroll
-    for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-            if (m0 + 4 * y + wave < a.M && n + 4 * p < a.N) base[y][p] = lowrank_load4<OUT>(a.base, static_cast<size_t>(m0 + 4 * y + wave) * a.N + n + 4 * p);
     Eight<DT> piece[STEPS][PIECES];
     int E = 14;
     if (leaders != 0) {  // uniform over the workgroup
@@ -456,31 +452,69 @@ __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
         E = lowrank_pieces<DT, STEPS, PIECES>(terms, piece);
         __syncthreads();
     }
+    const int first = n0 + 128 * wave;
+    const int P = a.r / 8, bits = (P & (P - 1)) == 0 ? P - 1 : 0, down = 4 - (31 - __builtin_clz(static_cast<unsigned>(P)));  // P <= 16
+    unsigned char* const rows = reinterpret_cast<unsigned char*>(&block[wave][0]);
+    v4f total[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) total[c] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (; leaders != 0; leaders &= leaders - 1) {
         const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(leaders));
-        const auto* const B = static_cast<const One<DT>*>(a.B) + static_cast<size_t>(adapter) * a.N * a.r;
-        constexpr int AT_ONCE = 8 / STEPS;  // products whose rows of B are under way at a time
+        const char* const B = static_cast<const char*>(a.B) + (static_cast<size_t>(adapter) * a.N + min(first, a.N - 1)) * a.r * 2;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(B), 0, max(0, min(128, a.N - first)) * a.r * 2, 0x00020000);
 #pragma unroll
         for (int c0 = 0; c0 < 8; c0 += AT_ONCE) {
             Eight<DT> b[AT_ONCE][STEPS];
+            if constexpr (STEPS == 1) {
 #pragma unroll
-            for (int c = 0; c < AT_ONCE; ++c) {
-                const auto* const row = B + static_cast<size_t>(min(n0 + 128 * wave + 16 * (c0 + c) + i, a.N - 1)) * a.r;
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s) b[c][s] = *reinterpret_cast<const Eight<DT>*>(row + min(32 * s + 8 * g, a.r - 8));
+                for (int c = 0; c < AT_ONCE; ++c) {
+                    const auto* const row = static_cast<const One<DT>*>(a.B) + (static_cast<size_t>(adapter) * a.N + min(first + 16 * c + i, a.N - 1)) * a.r;
+                    b[c][0] = *reinterpret_cast<const Eight<DT>*>(row + min(8 * g, a.r - 8));
+                }
+            } else {
+                for (int y = 0; y < (AT_ONCE * 16 * P + 63) / 64; ++y) {
+                    const int at = 64 * y + lane, row = at / P, place = at - row * P;
+                    lowrank_to_lds(from, rows + 1024 * y, ((16 * c0 + row) * P + (place ^ (row >> down & bits))) * 16);
+                }
+                __builtin_amdgcn_s_waitcnt(0);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int c = 0; c < AT_ONCE; ++c) {
-                v4f x = lowrank_product<DT, STEPS, PIECES>(a.r, g, b[c], piece);
-                if (mine == adapter) {  // an infinity in one request's adapter stays with that request
-                    if constexpr (DT == RCP_F16)
+                if constexpr (STEPS > 1)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = ldexpf(x[j], E - 14);
-                    *reinterpret_cast<v4f*>(&block[i * ROW + 128 * wave + 16 * (c0 + c) + 4 * g]) = x;
-                }
+                    for (int s = 0; s < STEPS; ++s) {
+                        const int row = 16 * c + i, p = min(4 * s + g, P - 1);
+                        b[c][s] = *reinterpret_cast<const Eight<DT>*>(rows + (row * P + (p ^ (row >> down & bits))) * 16);
+                    }
+                v4f x = lowrank_product<DT, STEPS, PIECES>(a.r, g, b[c], piece);
+                if constexpr (DT == RCP_F16)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = ldexpf(x[j], E - 14);
+                // an infinity in one request's adapter stays with that request
+                if constexpr (STEPS == 1) {
+                    if (mine == adapter) *reinterpret_cast<v4f*>(&block[wave][i * ROW + 16 * c + 4 * g]) = x;
+                } else
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) total[c0 + c][j] = mine == adapter ? x[j] : total[c0 + c][j];
+            }
+            if constexpr (STEPS > 1) {  // all read, before the next ones come
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(0);
             }
         }
     }
+    // rows wave, wave + 4, ... of the tile, eight outputs a lane
+    Raw4<OUT> base[4][2];
+    const int n = n0 + 8 * lane;
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            if (m0 + 4 * y + wave < a.M && n + 4 * p < a.N) base[y][p] = lowrank_load4<OUT>(a.base, static_cast<size_t>(m0 + 4 * y + wave) * a.N + n + 4 * p);
+    if constexpr (STEPS > 1)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) *reinterpret_cast<v4f*>(&block[wave][i * ROW + 16 * c + 4 * g]) = total[c];
     __syncthreads();
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
@@ -490,7 +524,7 @@ __global__ __launch_bounds__(256) void lowrank_many_out_kernel(LowrankArgs a)
         for (int p = 0; p < 2; ++p)
             if (m0 + row < a.M && n + 4 * p < a.N) {
                 float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (adds) *reinterpret_cast<v4f*>(v) = *reinterpret_cast<const v4f*>(&block[row * ROW + 8 * lane + 4 * p]);
+                if (adds) *reinterpret_cast<v4f*>(v) = *reinterpret_cast<const v4f*>(&block[lane >> 4][row * ROW + 8 * i + 4 * p]);
                 lowrank_add4<OUT>(base[y][p], v);
                 lowrank_store4<OUT>(a.out, static_cast<size_t>(m0 + row) * a.N + n + 4 * p, v);
             }
