@@ -10,10 +10,13 @@
 // lane has weights of; value codes come back transposed from LDS (ds_read_b64_tr_b8: eight rows of sixteen bytes, a lane gets a column).
 // A code becomes a binary16 number, exactly, half an instruction each.
 //
-// The query of a row is scaled by a power of two that puts its largest element at 2^13 .. 2^14: one binary16 number holds a 16-bit
-// query exactly down to 2^-28 of that; a binary32 query takes two (QP).  Weights are 2^(score - m) s' <= 2^14 in one binary16 number where the result has no
-// more than 8 or 11 bits itself, in two otherwise (PP); the reference m of a row is held against score + log2 s', so that a page of a large scale and
-// little attention does not push the others out of binary16, and moves only when a weight would leave the range.  Sums are binary32.
+// The query of a row enters scaled by a power of two.  One token a sequence: its largest element at 2^13 .. 2^14, as one binary16 number (a 16-bit query exactly
+// down to 2^-28 of that) or two (a binary32 query, QP).  Several tokens: 16-bit queries as two or three E4M3 pieces, which meet the codes as they are in one
+// product each of 64 elements; binary32 queries as pairs of binary16 numbers.
+// A weight is 2^(score + log2 s' - m), at most 2^14; the codes of a page then enter the sum of outputs as they are, and its scale the sum of weights as 1 / s'.  The
+// reference m of a row is so held against score + log2 s' that a page of a large scale and little attention does not push the others out of
+// binary16; it moves only when a weight would leave the range.  A weight is one binary16 number (an error of 2^-11 at most, as the result's own for binary16 and
+// less than that for bfloat16), or two (PP): for binary32 results, and with one token a sequence, where the matrix cores wait anyway, for binary16 ones.  Sums are binary32.
 #include <math.h>
 
 #include <type_traits>
@@ -140,7 +143,9 @@ __device__ __forceinline__ void kv8_to_lds_once(__amdgpu_buffer_rsrc_t from, uns
 // ---------------------------------------------------------------------------------------
 // One new token a sequence.  Workgroup = one wavefront = (chunk of cached tokens of a sequence, cache head [, sixteen of its query heads]); the chunks are
 // cut on the device from the lengths, so that a captured call stays balanced when they change.  16x16x32 products: a lane holds the row (query
-// head) lane % 16.
+// head) lane % 16.  Bound by the reads of codes: 103 MB (16 sequences of up to 6000 tokens, 8 heads of 128) in 23.6 us, 4.4 TB/s, and 4.6 us for the merge; 33 MB (one
+// sequence, 32 heads) in 10.8 us, of which half are the start and the chain length -> page -> codes.  Why a wavefront a workgroup: with four and a common
+// chunk, a barrier in each tile made all wait for the slowest load (31.5 us instead of 28, merge included).
 // ---------------------------------------------------------------------------------------
 
 // which 16-byte piece of a token's value codes stands at place p of its row in LDS: p ^ this; the rows that a transposing read takes together
@@ -434,7 +439,10 @@ __global__ __launch_bounds__(GROUPS * D) void kv8_decode_merge_kernel(Kv8AttnArg
 // ---------------------------------------------------------------------------------------
 // Several new tokens a sequence, each of which sees the tokens up to its own.  Workgroup = (128 rows of a sequence and cache head, [part of
 // the cached tokens]); row = (new token, query head of the group).  32x32x16 products: a lane holds the row lane % 32 of its
-// wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS.
+// wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS, four of them, of which
+// three are under way.  Bound by the vector unit (a conversion to binary16, a multiply-add, an exponential, a rounding, the maximum and the sum of each
+// score and value) and the matrix cores together: some 1400 and 1000 of a tile's 2400 cycles, which hardly overlap.  8192 tokens of 32 + 2 x 8 heads of
+// 128: 550 GFLOP in 534 .. 600 us, 0.9 .. 1.0 PFLOP/s; four prompts of 301 to 2000 tokens 56 GFLOP in 87 .. 97 us.
 // ---------------------------------------------------------------------------------------
 constexpr int KV8_ROWS = 128;
 constexpr int KV8_STAGES = 4;  // tiles in LDS: one in use, the others under way

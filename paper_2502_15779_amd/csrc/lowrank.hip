@@ -64,7 +64,8 @@ __device__ __forceinline__ unsigned long long lowrank_leaders(int id, int tokens
 }
 
 // Few tokens: workgroup = (split of K, slot of leaders, sixteen tokens); each wavefront sums a quarter of the split, from registers, two blocks of
-// two steps ahead of the products (rows = ranks, columns = tokens).
+// two steps ahead of the products (rows = ranks, columns = tokens).  Bound by the launch and the chain adapter -> rows: 16 tokens with an adapter each, K = 4096,
+// r = 16: 4.5 us for 2.2 MB; one token, K = 2048, r = 8: 2.6 us.
 template <int DT, int NR>
 __global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
 {
@@ -350,7 +351,8 @@ __device__ __forceinline__ v4f lowrank_product(int r, int g, Eight<DT> (&b)[STEP
 }
 
 // Few tokens, so that many have an adapter of their own: workgroup = (32 outputs, sixteen tokens); wavefront w takes the adapters w, w + 4, ... of the tile and
-// writes the rows of their tokens.  Products with rows = outputs, columns = tokens: a lane holds token lane % 16 and four neighbouring outputs.
+// writes the rows of their tokens.  Products with rows = outputs, columns = tokens: a lane holds token lane % 16 and four neighbouring outputs.  16 tokens beside
+// 12288 outputs, r = 16: 5.3 us for 7 MB; one token beside 2048: 3.6 us, again the launch and a chain of loads.
 template <int DT, int OUT, int STEPS>
 __global__ __launch_bounds__(256) void lowrank_few_out_kernel(LowrankArgs a)
 {
