@@ -440,7 +440,7 @@ __global__ __launch_bounds__(GROUPS * D) void kv8_decode_merge_kernel(Kv8AttnArg
 // Several new tokens a sequence, each of which sees the tokens up to its own.  Workgroup = (128 rows of a sequence and cache head, [part of
 // the cached tokens]); row = (new token, query head of the group).  32x32x16 products: a lane holds the row lane % 32 of its
 // wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS, four of them, of which
-// three are under way.  Bound by the vector unit (a conversion to binary16, a multiply-add, an exponential, a rounding, the maximum and the sum of each
+// three are under way (the compiler waits for them before the transposing reads; loads behind those reads measure the same).  Bound by the vector unit (a conversion to binary16, a multiply-add, an exponential, a rounding, the maximum and the sum of each
 // score and value) together with the matrix cores: busy 68 and 47 % of the cycles.  8192 tokens of 32 + 2 x 8 heads of 128: 550 GFLOP in 538 .. 592 us, 0.93 ..
 // 1.02 PFLOP/s; four prompts of 301 to 2000 tokens 56 GFLOP in 86 .. 98 us.
 // ---------------------------------------------------------------------------------------

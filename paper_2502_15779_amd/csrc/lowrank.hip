@@ -141,7 +141,8 @@ __global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
 
 // Many tokens: workgroup = (split of K, slot of leaders, 64 tokens), sixteen tokens of each wavefront.  Bound by the memory x comes from (2001 tokens, K = 14336,
 // r = 64, bfloat16: 57 MB in 18.8 us, 3.1 TB/s).  x and A come through LDS in stages of 64 columns, so that the four wavefronts share A and a load takes 128 bytes
-// of a row; three stages, so that two are under way (two stages: as fast there).  Piece p (16 bytes) of row n stands at place p ^ (n / 2 % 8): the sixteen
+// of a row.  (The compiler waits for all loads into LDS before a read of it, so that the overlap is between the workgroups of a compute unit; two stages, or
+// loads behind the reads, measure the same.)  Piece p (16 bytes) of row n stands at place p ^ (n / 2 % 8): the sixteen
 // rows that are read together, 128 bytes each, fall into different banks.
 constexpr int LOWRANK_STAGE = 64, LOWRANK_STAGES = 3;
 
