@@ -101,6 +101,23 @@ def test_an_infinity_stays_with_its_request(M):
     assert torch.equal(got[keep], want[keep])
 
 
+@pytest.mark.parametrize("M,N,K,r,adapters,dtype,out", [
+    (129, 1028, 64, 64, 3, "bf16", "bf16"), (100, 516, 96, 40, 100, "f16", "f32"), (66, 1140, 32, 48, 2, "bf16", "f16"), (77, 36, 160, 96, 9, "f16", "f16"),
+    (81, 640, 64, 112, 2, "bf16", "f32"), (70, 4, 64, 56, 5, "f16", "bf16")])
+def test_many_tokens_and_ranks(M, N, K, r, adapters, dtype, out):
+    """Rows of B of every number of pieces, wavefronts whose outputs end early or are none, tiles of many adapters; infinities and NaN stay with their adapter."""
+    print("ranks", M, N, K, r, adapters, dtype, out, flush=True)
+    g, x, A, B, scaling, base = _inputs(5 * M + r, M, N, K, r, adapters, dtype, out)
+    which = torch.randint(-1, adapters, (M,), generator=g)
+    which[:2] = torch.tensor([0, 1])
+    got = _run(x, A, B, which, scaling, base)
+    _check(x, A, B, which, scaling, base, got)
+    B[1, :, 3] = float("inf")
+    A[1, 5] = float("nan")
+    other = _run(x, A, B, which, scaling, base)
+    assert torch.equal(other[which != 1], got[which != 1]) and not bool(other[1].isfinite().any())
+
+
 @pytest.mark.parametrize("size", [1e-4, 1.0, 60000.0])
 def test_magnitudes(size):
     """Inner products far from 1: binary16 operands are scaled per token."""
