@@ -140,15 +140,35 @@ __global__ __launch_bounds__(256) void lowrank_few_in_kernel(LowrankArgs a)
 }
 
 // Many tokens: workgroup = (split of K, slot of leaders, 64 tokens), sixteen tokens of each wavefront.  Bound by the memory x comes from (2001 tokens, K = 14336,
-// r = 64, bfloat16: 57 MB in 18.8 us, 3.1 TB/s).  x and A come through LDS in stages of 64 columns, so that the four wavefronts share A and a load takes 128 bytes
-// of a row.  (The compiler waits for all loads into LDS before a read of it, so that the overlap is between the workgroups of a compute unit; two stages, or
-// loads behind the reads, measure the same.)  Piece p (16 bytes) of row n stands at place p ^ (n / 2 % 8): the sixteen
-// rows that are read together, 128 bytes each, fall into different banks.
+// r = 64, bfloat16: 57 MB in 16.8 us, 3.4 TB/s).  x and A come through LDS in stages of 64 columns, so that the four wavefronts share A and a load takes 128 bytes
+// of a row; three stages, two under way while one is multiplied (18.7 us with all loads ended before each read; four and five stages measure the same).  Piece p
+// (16 bytes) of row n stands at place p ^ (n / 2 % 8): the sixteen rows that are read together, 128 bytes each, fall into different banks.
 constexpr int LOWRANK_STAGE = 64, LOWRANK_STAGES = 3;
 
 __device__ __forceinline__ void lowrank_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* to, int offset)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint32_t lowrank_lds(const unsigned char* p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p));
+}
+
+// One 16-byte piece of a token and NR pieces of sixteen ranks each, 2048 bytes apart, out of LDS; they have arrived when this returns.  (Written out, because the
+// compiler lets all loads into LDS end before a read of its own there.)
+template <int NR>
+__device__ __forceinline__ void lowrank_read(uint32_t x, uint32_t a, u32x4& xv, u32x4 (&av)[NR])
+{
+    if constexpr (NR == 1)
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(xv), "=&v"(av[0]) : "v"(x), "v"(a) : "memory");
+    else if constexpr (NR == 2)
+        asm volatile("ds_read_b128 %0, %3\n\tds_read_b128 %1, %4\n\tds_read_b128 %2, %4 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(xv), "=&v"(av[0]), "=&v"(av[1]) : "v"(x), "v"(a) : "memory");
+    else
+        asm volatile("ds_read_b128 %0, %5\n\tds_read_b128 %1, %6\n\tds_read_b128 %2, %6 offset:2048\n\tds_read_b128 %3, %6 offset:4096\n\t"
+                     "ds_read_b128 %4, %6 offset:6144\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(xv), "=&v"(av[0]), "=&v"(av[1]), "=&v"(av[2]), "=&v"(av[3]) : "v"(x), "v"(a) : "memory");
 }
 
 template <int DT, int NR>
@@ -197,7 +217,9 @@ __global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
                 // this wavefront's part of the stage is in LDS once only the later ones' loads are outstanding,
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(((X_LOADS + A_LOADS) * (LOWRANK_STAGES - 2)) | (7 << 4) | (15 << 8));
-                __syncthreads();  // then everybody's is, and the stage before has been read
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_barrier();  // then everybody's is, and the stage before has been read: reads wait for themselves
+                asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
                 stage(k + LOWRANK_STAGE * (LOWRANK_STAGES - 1), buf == 0 ? LOWRANK_STAGES - 1 : buf - 1);
                 __builtin_amdgcn_sched_barrier(0);
@@ -205,10 +227,10 @@ __global__ __launch_bounds__(256) void lowrank_many_in_kernel(LowrankArgs a)
                 for (int s = 0; s < LOWRANK_STAGE / LOWRANK_STEP; ++s) {
                     if (k + LOWRANK_STEP * s >= k1) break;  // uniform
                     const int at = ((4 * s + g) ^ (i >> 1)) * 16;
-                    const Eight<DT> xv = *reinterpret_cast<const Eight<DT>*>(&xs[buf][(16 * wave + i) * ROW + at]);
+                    u32x4 xv, av[NR];
+                    lowrank_read<NR>(lowrank_lds(&xs[buf][(16 * wave + i) * ROW + at]), lowrank_lds(&as[buf][i * ROW + at]), xv, av);
 #pragma unroll
-                    for (int n = 0; n < NR; ++n)
-                        acc[n] = lowrank_mfma<DT>(*reinterpret_cast<const Eight<DT>*>(&as[buf][(16 * n + i) * ROW + at]), xv, acc[n]);
+                    for (int n = 0; n < NR; ++n) acc[n] = lowrank_mfma<DT>(__builtin_bit_cast(Eight<DT>, av[n]), __builtin_bit_cast(Eight<DT>, xv), acc[n]);
                 }
                 buf = buf == LOWRANK_STAGES - 1 ? 0 : buf + 1;
             }
