@@ -194,8 +194,13 @@ def run(s):
                            rope=s["rope"], rotate=s["rotate"], q=s["q"], q_out=s["q_out"])
             return [s["kc"], s["ks"], s["vc"], s["vs"], s["q_out"]]
         if s["kind"] == "attn":
+            work = s["work"]
+            if s["starts"] is not None:   # rows that are split can take more than the scratch: such a call makes its own
+                n, hq, d = s["q"].shape
+                need = rcp.kv8_workspace_bytes(n, s["lengths"].numel(), hq, s["kc"].shape[1], d, False)
+                work = work if need <= work.numel() else None
             return rcp.kv8_attn(s["q"], s["lengths"], s["table"], s["kc"], s["ks"], s["vc"], s["vs"], s["scale"], starts=s["starts"],
-                                out=s["out"], workspace=s["work"])
+                                out=s["out"], workspace=work)
         return rcp.lowrank_add(s["x"], s["A"], s["B"], s["which"], s["scaling"], s["base"], out=s["out"], workspace=s["work"])
     return {"append": _plain_append, "attn": _plain_attn, "lowrank": _plain_lowrank}[s["kind"]](s)
 
