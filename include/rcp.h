@@ -594,8 +594,8 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
  *   q: [rows][H_q][D] of `q_dtype`; out: [rows][H_q][D] of `out_dtype` (any rcp_dtype).  A row that sees no token (an empty sequence, no
  *   page) gets zeros.  softmax_scale: finite and not negative (RCP_ERR_UNSUPPORTED).  Tokens behind a row's own never enter, whatever bytes their slots hold; codes within a sequence must not be NaN
  *   (rcp_kv8_append writes none).  Scales count as 2^-40 .. 2^120, a smaller one (0 of a page never written) as 2^-40.  Scores have to stay within binary32.  Sums
- *   are binary32.  The softmax weights enter the product with the values as binary16 numbers, or as pairs of them (22 bits) for binary32 results and, with one
- *   token a sequence, binary16 ones.  A row's query enters scaled by its largest element: 16-bit ones exactly down to 2^-28 of that with one token a
+ *   are binary32.  The softmax weights enter the product with the values as pairs of binary16 numbers (22 bits), with several tokens and bfloat16
+ *   results as one (11 bits).  A row's query enters scaled by its largest element: 16-bit ones exactly down to 2^-28 of that with one token a
  *   sequence, otherwise off by 2^-23 of it (bfloat16) or 2^-28 (binary16) at most; binary32 ones as pairs of binary16 numbers.  out must not overlap q.
  *   workspace: rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, starts == NULL) bytes, overwritten by every call.  Calls that
  *   may overlap need workspaces of their own.

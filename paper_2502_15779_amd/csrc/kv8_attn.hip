@@ -15,8 +15,11 @@
 // product each of 64 elements; binary32 queries as pairs of binary16 numbers.
 // A weight is 2^(score + log2 s' - m), at most 2^14; the codes of a page then enter the sum of outputs as they are, and its scale the sum of weights as 1 / s'.  The
 // reference m of a row is so held against score + log2 s' that a page of a large scale and little attention does not push the others out of
-// binary16; it moves only when a weight would leave the range.  A weight is one binary16 number (an error of 2^-11 at most, as the result's own for binary16 and
-// less than that for bfloat16), or two (PP): for binary32 results, and with one token a sequence, where the matrix cores wait anyway, for binary16 ones.  Sums are binary32.
+// binary16; it moves only when a weight would leave the range.  A weight enters the product as two binary16 numbers, 22 bits of it.  One number (PP = 1) is off by up to
+// 2^-11 of the weight, and only several tokens with bfloat16 results, whose own half step is 2^-8, take it: there the second product of each block costs a third (8192 tokens of 32 + 2 x 8 heads
+// of 128: 541 us with one number, 738 with two) and changes the error against 64 bits by less than a hundredth.  For binary16 results it would be as large as the result's own rounding,
+// and more where values cancel (three chunks behind 5000 to 17003 tokens, heads of 64: 62 us and an error of 2.4e-4 with one, 80 us and 2.1e-4 with two); single
+// tokens hardly pay for it (16 sequences of up to 6000 tokens 27.4 us with one, 28.3 with two).  Sums are binary32.
 #include <math.h>
 
 #include <type_traits>
@@ -176,7 +179,7 @@ __device__ __forceinline__ Kv8Chunk kv8_chunk(const Kv8Table& t, int chunks, int
     return {b, __builtin_amdgcn_readfirstlane(length_of(b)), __builtin_amdgcn_readfirstlane(u.within), C};
 }
 
-template <int D, int QP, int PP>
+template <int D, int QP>
 __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 {
     constexpr int KX = D / 64;  // 16-byte loads of a lane for sixteen tokens' keys
@@ -314,7 +317,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) acc[d] *= alpha;
         }
-        v8h ph[2], pl[PP == 2 ? 2 : 1];
+        v8h ph[2], pl[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             float w[8];
@@ -326,7 +329,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
             l = fmaf((w[0] + w[1]) + (w[2] + w[3]), vs[2 * s], l);
             l = fmaf((w[4] + w[5]) + (w[6] + w[7]), vs[2 * s + 1], l);
             ph[s] = kv8_round(w);
-            if constexpr (PP == 2) pl[s] = kv8_rest(w, ph[s]);
+            pl[s] = kv8_rest(w, ph[s]);
         }
         // the values of this tile are in LDS once no more loads than the keys requested above are outstanding
         __builtin_amdgcn_sched_barrier(0);
@@ -344,7 +347,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
                 const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                     (__attribute__((address_space(3))) v2i*)(vat + 32 * s * D + ((d ^ f) * 16)));
                 const v8h v = kv8_halves(static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]));
-                if constexpr (PP == 2) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[s], acc[d], 0, 0, 0);
+                acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pl[s], acc[d], 0, 0, 0);
                 acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, ph[s], acc[d], 0, 0, 0);
             }
         // every read of the tile has returned before the next one overwrites it
@@ -809,15 +812,12 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
         if (one) {
             const dim3 grid(static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv), static_cast<unsigned>((a.rep + 15) / 16));
             auto launch = [&](auto kernel) { enqueue(kernel, grid, 64, 0, st, a); };
-            const bool p2 = c.out_dtype != RCP_BF16;
-            if (q2 && p2) launch(&kv8_decode_kernel<D, 2, 2>);
-            else if (q2) launch(&kv8_decode_kernel<D, 2, 1>);
-            else if (p2) launch(&kv8_decode_kernel<D, 1, 2>);
-            else launch(&kv8_decode_kernel<D, 1, 1>);
+            if (q2) launch(&kv8_decode_kernel<D, 2>);
+            else launch(&kv8_decode_kernel<D, 1>);
         } else {
             const unsigned grid = static_cast<unsigned>(plan.tiles) * static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv);
             auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
-            const bool p2 = c.out_dtype == RCP_F32;
+            const bool p2 = c.out_dtype != RCP_BF16;
             if (q2 && p2) launch(&kv8_prompt_kernel<D, 0, 2>);
             else if (q2) launch(&kv8_prompt_kernel<D, 0, 1>);
             else if (c.q_dtype == RCP_F16 && p2) launch(&kv8_prompt_kernel<D, 3, 2>);
