@@ -48,3 +48,34 @@ def test_values_that_cancel(D, one, out, weight):
     off = (got - exact).abs()
     assert bool((exact.abs() < 0.05 * mag).any())
     assert bool((off <= tol).all()), f"{float((off / tol).max()):.2f} of what is allowed"
+
+
+@pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("out,low,high", [("f16", -20, 3), ("f16", -22, 6), ("bf16", -20, 6), ("bf16", -30, 6), ("f32", -20, 3), ("f32", -22, 6), ("f32", -40, 10)])
+def test_values_of_very_different_size_that_are_attended_to_alike(one, out, low, high):
+    """Pages of values 2^23 to 2^50 apart whose tokens have weights of the same size, the large page zero in half of its elements: what stands there comes from
+    weights that, with their page's scale, are subnormal binary16 numbers or none.  A weight times its scale is then off by up to 2^-34 of the row's largest one (2^-25 where that is
+    2^9 or more), and no element by more than the sum of that over the tokens."""
+    D, page, rep = 64, 16, 2
+    g = torch.Generator().manual_seed(high - low)
+    kc = torch.randn((3, 1, page, D), generator=g).to(ref.E4M3)
+    vc = (torch.randn((3, 1, page, D), generator=g) * 60).clamp(-448, 448).to(ref.E4M3)
+    vc[1, :, :, ::2] = torch.zeros_like(vc[1, :, :, ::2])
+    ks, vs = torch.full((3, 1), 1.0), torch.tensor([[2.0 ** low], [2.0 ** high], [2.0 ** (low + 3)]])
+    q = (0.5 * torch.randn((3, rep, D), generator=g)).to(DTYPES[out])
+    lengths, starts, table = ([48, 40, 34], None, _int([[0, 1, 2], [2, 1, 0], [1, 0, 2]])) if one else ([48], [0, 3], _int([[0, 1, 2]]))
+    got, (exact, mag, size, seen) = _run(q, lengths, starts, table, [kc, ks, vc, vs], 0.2, DTYPES[out])
+    floor = torch.zeros_like(exact)
+    for i in range(3):
+        n, ids = (lengths[i], table[i]) if one else (46 + i, table[0])
+        at, slots = ids.long().repeat_interleave(page)[:n], torch.arange(n) % page
+        for h in range(rep):
+            p = torch.softmax(0.2 * (kc[at, 0, slots].double() @ q[i, h].double()), 0) * vs[at, 0].double()
+            floor[i, h] = 2.0 ** -34 * p.max() * vc[at, 0, slots].double().abs().sum(0)
+    weight = 2.0 ** -11 if out == "bf16" and not one else 2.0 ** -22
+    e = (weight + 2 * ((D + 16) * 2.0 ** -24 + (2.0 ** -21 if out == "f32" else 0.0)) * size + (seen + 16) * 2.0 ** -24) * 2 * mag
+    tol = e + floor + torch.finfo(DTYPES[out]).eps / 2 * exact.abs() + (2.0 ** -25 if out == "f16" else 0.0)
+    off = (got - exact).abs()
+    assert bool((off <= tol).all()), f"{float((off / tol).max()):.2f} of what is allowed"
+    if high - low >= 46:
+        assert bool((off > e).any()), "the range of the weights does not show here"
