@@ -21,7 +21,7 @@
 // and more where values cancel (three chunks behind 5000 to 17003 tokens, heads of 64: 62 us and an error of 2.4e-4 with one, 80 us and 2.1e-4 with two); single
 // tokens hardly pay for it (16 sequences of up to 6000 tokens 27.4 us with one, 28.3 with two).  The range of binary16 ends below, too: with a row's largest weight at
 // 2^9 .. 2^14, one number has its 11 bits down to 2^-23 of that (two their 22 bits down to 2^-12), and either form is off by 2^-34 of it at most.  Since a weight carries its page's
-// scale, this can only show in elements that are zero in all pages of large values beside pages of values 2^12, or 2^23, times smaller.  Sums are binary32.
+// scale, this can only show in elements that are zero in all tokens of a large weight times scale, beside tokens 2^12, or 2^23, times smaller.  Sums are binary32.
 #include <math.h>
 
 #include <type_traits>
