@@ -600,7 +600,8 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
  *   sequence, otherwise off by 2^-23 of it (bfloat16) or 2^-28 (binary16) at most; binary32 ones as pairs of binary16 numbers.  out must not overlap q.
  *   workspace: rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, starts == NULL) bytes, overwritten by every call.  Calls that
  *   may overlap need workspaces of their own.
- * Limits: sequences <= 1024, sequences * width * page < 2^31, H_q <= 4096, rows <= 2^20 (RCP_ERR_SHAPE).
+ * Limits (RCP_ERR_SHAPE): sequences <= 1024, width * page <= 2^24, sequences * width * page < 2^31, H and H_q <= 4096, rows <= 2^20; rcp_kv8_append: strides <= 2^31,
+ * 2 H (rows / page + 2 sequences + 8) + rows H_q < 2^31; rcp_kv8_attn: (rows (H_q / H) / 128 + sequences) H < 2^24.
  */
 typedef struct {
     void* k_codes;

@@ -826,7 +826,8 @@ int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const v
     if (!q || !out) return fail(RCP_ERR_NULL, "%s: NULL pointer argument", fn);
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(RCP_ERR_ALIGN, "%s: device buffers must be 16-byte aligned", fn);
     const bool one = batch->starts_or_null == nullptr;
-    if ((static_cast<long long>(batch->rows) * (H_q / cache->H) / 128 + batch->sequences) * cache->H > 0x7fffffffLL / 32)
+    // a workgroup of 256 threads for each tile of 128 rows, and a grid takes fewer than 2^32 threads (what is split besides is far fewer)
+    if ((static_cast<long long>(batch->rows) * (H_q / cache->H) / 128 + batch->sequences) * cache->H >= 1LL << 24)
         return fail(RCP_ERR_SHAPE, "%s: %d rows of %d heads are too many", fn, batch->rows, H_q);
     const size_t need = kv8_workspace_bytes(batch->rows, batch->sequences, H_q, cache->H, cache->D, one);
     if (workspace == nullptr || workspace_bytes < need)

@@ -15,6 +15,8 @@
 namespace rcp {
 
 constexpr int KV8_QUERIES = 4;  // query vectors of a lane in a prompt
+// A dimension of a grid ends below 2^32 threads, which are 2^24 workgroups of 256: a longer one is folded into rows of 2^23.
+constexpr int KV8_GRID_SHIFT = 23;
 
 struct Kv8AppendArgs {
     Kv8Table t;
@@ -26,6 +28,7 @@ struct Kv8AppendArgs {
     float *k_scales, *v_scales;
     int rows, H, H_q, rotate;
     int kv_groups;                           // workgroups that write pages; those behind them rotate queries
+    int groups;                              // of both
 };
 
 template <int CTRL>
@@ -264,14 +267,15 @@ __global__ __launch_bounds__(256) void kv8_append_pages_kernel(Kv8AppendArgs a)
 {
     constexpr int LANES = D / 8, ROWS = 256 / LANES;
     __shared__ uint32_t red[4];
-    if (static_cast<int>(blockIdx.x) >= a.kv_groups) {
-        kv8_queries<DT, D, KV8_QUERIES>(a, blockIdx.x - a.kv_groups);
+    const int block = static_cast<int>(blockIdx.y << KV8_GRID_SHIFT | blockIdx.x);
+    if (block >= a.kv_groups) {
+        if (block < a.groups) kv8_queries<DT, D, KV8_QUERIES>(a, block - a.kv_groups);
         return;
     }
     // Workgroups go to the eight dies in turn; a die gets all heads of a page one after the other, since they read the same angles (7273 tokens
     // of 32 + 2 x 8 heads of 128 42.4 us, with a die to each head 44.5; without a position rotation 36.9 and 36.4).
-    const int eighth = static_cast<int>(blockIdx.x) >> 3, round = eighth / (2 * a.H), part = eighth - round * 2 * a.H;
-    const int unit_of = 8 * round + (static_cast<int>(blockIdx.x) & 7);
+    const int eighth = block >> 3, round = eighth / (2 * a.H), part = eighth - round * 2 * a.H;
+    const int unit_of = 8 * round + (block & 7);
     const bool values = part >= a.H;
     const int h = values ? part - a.H : part;
     const int tid = threadIdx.x, lane = tid & 63, l = tid % LANES;
@@ -354,7 +358,9 @@ int launch_kv8_append(const Kv8AppendCall& c, hipStream_t st)
                       : static_cast<int>((kv8_most_pages(c.rows, c.sequences, c.shift) + 7) / 8 * 8) * 2 * c.H;
     const int q_vectors = one ? vectors : KV8_QUERIES * vectors;
     const long long q_groups = (static_cast<long long>(c.rows) * a.H_q + q_vectors - 1) / q_vectors;
-    const unsigned grid = static_cast<unsigned>(a.kv_groups + q_groups);
+    a.groups = a.kv_groups + static_cast<int>(q_groups);
+    const unsigned row = 1u << KV8_GRID_SHIFT, groups = static_cast<unsigned>(a.groups);
+    const dim3 grid = groups <= row ? dim3(groups) : dim3(row, (groups + row - 1) / row);
     auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
     const int passes = (c.D << c.shift) / 2048;  // vectors a lane for a whole page: 0 (half a pass), 1, 2, 4, 8
 #define RCP_KV8_APPEND(DT, D)                                                   \
