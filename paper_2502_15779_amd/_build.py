@@ -23,14 +23,12 @@ COMPILE_FLAGS = [
     # kernel arguments arrive in scalar registers with the wavefront launch instead of being
     # fetched by its first instructions (these kernels run for a few microseconds)
     "-mllvm", "-amdgpu-kernarg-preload-count=16",
+    # results of matrix instructions in ordinary vector registers: kept in accumulation registers, this compiler (clang 22,
+    # ROCm 7.2) has read them without the wait that the hardware needs where a loop of one such instruction ends
+    # (`v_accvgpr_read` of the last product: its sum was the one before)
+    "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-Wall", "-Wno-unused-command-line-argument",
 ]
-
-
-# Results of matrix instructions in ordinary vector registers.  Kept in accumulation registers, this compiler (clang 22, ROCm 7.2) reads them without the
-# wait that the hardware needs where a loop of one such instruction ends (`v_accvgpr_read` of the last product: its sum was the one before).
-_MFMA_VGPRS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-FILE_FLAGS = {"kv8_attn.hip": _MFMA_VGPRS, "lowrank.hip": _MFMA_VGPRS}
 
 
 def sources():
@@ -61,7 +59,7 @@ def build(verbose: bool = False, jobs: int = 0) -> str:
     try:
         srcs = sources()
         objs = [os.path.join(tmp, os.path.basename(s)[:-4] + ".o") for s in srcs]
-        cmds = [[hipcc] + COMPILE_FLAGS + FILE_FLAGS.get(os.path.basename(s), []) + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", s, "-o", o]
+        cmds = [[hipcc] + COMPILE_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", s, "-o", o]
                 for s, o in zip(srcs, objs)]
         host_obj = os.path.join(tmp, "binding.host.o")
         host_cmd, torch_lib = _host_command(host_obj)
