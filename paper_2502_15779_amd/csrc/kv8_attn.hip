@@ -11,7 +11,7 @@
 // A code becomes a binary16 number, exactly, half an instruction each.
 //
 // The query of a row enters scaled by a power of two.  One token a sequence: its largest element at 2^13 .. 2^14, as one binary16 number (a 16-bit query exactly
-// down to 2^-28 of that) or two (a binary32 query, QP).  Several tokens: 16-bit queries as two or three E4M3 pieces, which meet the codes as they are in one
+// down to 2^-27 of that) or two (a binary32 query, QP).  Several tokens: 16-bit queries as two or three E4M3 pieces, which meet the codes as they are in one
 // product each of 64 elements; binary32 queries as pairs of binary16 numbers.
 // A weight is 2^(score + log2 s' - m), at most 2^14; the codes of a page then enter the sum of outputs as they are, and its scale the sum of weights as 1 / s'.  The
 // reference m of a row is so held against score + log2 s' that a page of a large scale and little attention does not push the others out of
@@ -459,9 +459,9 @@ __device__ __forceinline__ int kv8_prompt_swizzle(int token)
     else return ((token >> 2) & 1) | ((token >> 2) & 2);
 }
 
-// v in units of 2^-8 of its row's largest element's binade, as `PIECES` E4M3 numbers, each of 2^-5 times the unit of the one before: four bits and
+// v, scaled so that its row's largest element is at 2^7 .. 2^8, as `PIECES` E4M3 numbers, each of 2^-5 times the unit of the one before: four bits and
 // the sign of the rest each, so that two hold a bfloat16 number and three a binary16 number exactly, down to 2^-14 of the largest; below that the
-// rest is at most 2^-18 of it with one piece, 2^-23 with two, 2^-28 with three.  Four numbers to a dword of each piece.
+// rest is at most 2^-15 with two pieces and 2^-20 with three: 2^-22 and 2^-27 of a largest element of 2^7.  Four numbers to a dword of each piece.
 template <int PIECES>
 __device__ __forceinline__ void kv8_query_pieces(const float (&v)[4], int (&piece)[PIECES])
 {
