@@ -632,7 +632,7 @@ int rcp_kv8_attn(const rcp_kv8_cache* cache, const rcp_kv8_batch* batch, const v
  * x: [M][K]; A: [adapters][r][K]; B: [adapters][N][r], all of `x_dtype` (RCP_F16 or RCP_BF16).  which: int32 [M] on the device; an entry
  * outside 0 .. adapters - 1 is no adapter: out[m] = base[m].  scaling: binary32 [adapters].  base, out: [M][N] of `out_dtype` (any
  * rcp_dtype); out may be base itself.  The inner product x A^T is held in binary32 (sums in a fixed order) and multiplied by B with
- * at least 22 bits.  r a multiple of 8 up to RCP_LOWRANK_MAX_R, K a multiple of 32 up to 2^20, N of 4 up to 2^24 (RCP_ERR_SHAPE).
+ * 24 bits (bfloat16), or 22 bits down to 2^-16 of the token's largest, off by 2^-38 of that below (binary16).  r a multiple of 8 up to RCP_LOWRANK_MAX_R, K a multiple of 32 up to 2^20, N of 4 up to 2^24 (RCP_ERR_SHAPE).
  * workspace: rcp_lowrank_workspace_bytes(M, N, K, r) bytes, overwritten by every call.
  */
 #define RCP_LOWRANK_MAX_R 128

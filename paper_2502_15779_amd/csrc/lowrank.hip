@@ -6,8 +6,8 @@
 // sums go to the workspace, in binary32 and in a fixed order (no atomics).  The second adds them up and multiplies by B.  A tile of
 // tokens is multiplied once for each adapter that one of its tokens has (a "leader" is the first token of the tile with that adapter), and
 // a token keeps the products of its own one.
-// t has 32 bits and the matrix cores take 16: it goes in as two binary16 numbers, scaled by a power of two per token (22 bits and more
-// of every value down to 2^-12 of the token's largest), or as three bfloat16 numbers (24 bits).
+// t has 32 bits and the matrix cores take 16: it goes in as two binary16 numbers, scaled by a power of two per token (22 bits
+// of every value down to 2^-16 of the token's largest, smaller ones off by 2^-38 of that at most), or as three bfloat16 numbers (24 bits).
 #include <type_traits>
 
 #include "rcp_internal.hpp"
