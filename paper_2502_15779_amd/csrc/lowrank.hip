@@ -562,12 +562,18 @@ struct LowrankPlan {
     int tiles, chunk, splits, slots;  // of the first kernel
 };
 
+// Which kernels: the host does not see how many adapters a tile has.  Those of few tokens are ahead by far with an adapter each, those of many with one for all, and the second
+// difference grows with the outputs.  4096 x 4096, rank 16, bfloat16, few and many: 128 tokens of one adapter 7.5 and 8.6 us, of an adapter each 14 and 60; 256 tokens 9.9 and 8.8, 25 and 60.
+// 14336 x 4096, rank 16: 128 tokens 12.3 and 9.0, 24 and 61; 256 tokens 19.6 and 9.9, 43 and 63.
+// Splits: 512 columns and more (one token of 4096 columns, both kernels: 5.9 us; 256 and more 6.4, 1024 and more 6.4; 16 tokens of an adapter each 8.9, 9.4, 9.7).
+// Leaders side by side: sixteen for few tokens, as many as a tile has (16 tokens of an adapter each, 4096 x 4096: 8.9 us; 8 10.1, 4 12.7); four for many (2001 tokens of five adapters
+// beside 14336 columns 36.4 us; 2 36.6, 16 39.5, 1 37.5; but 300 tokens of an adapter each 61, 93, 41, 160).
 static LowrankPlan lowrank_plan(int M, int K)
 {
     LowrankPlan p;
-    p.many = M > 64;
+    p.many = M > 128;
     p.tiles = p.many ? (M + 63) / 64 : (M + 15) / 16;
-    const int least = 512, most = (K + least - 1) / least;  // splits of 512 columns and more
+    const int least = 512, most = (K + least - 1) / least;
     int splits = 2 * num_compute_units() / p.tiles;
     splits = splits < 1 ? 1 : splits > most ? most : splits;
     const int unit = p.many ? LOWRANK_STAGE : least;
