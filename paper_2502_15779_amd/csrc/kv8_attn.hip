@@ -762,6 +762,8 @@ static Kv8AttnPlan kv8_attn_plan(int rows, int sequences, int H_q, int H_kv, int
     const int cus = num_compute_units(), rep = H_q / H_kv;
     const size_t partial = static_cast<size_t>(H_q) * (D + KV8_EXTRA) * sizeof(float);
     if (one) {
+        // Eight wavefronts a compute unit, two a SIMD (heads of 128): 13.0 us for one sequence of 4001 tokens of 32 heads, 27.6 for 16 of up to 6000 tokens of 32 over 8 heads.
+        // With four 14.2 and 29.9, with sixteen 13.3 and 30.9; one sequence of 30000 tokens of 8 heads 22.7, with four 20.5, with sixteen 31.3.
         p.chunks = 8 * cus / H_kv > 2 * sequences ? 8 * cus / H_kv : 2 * sequences;
         p.tiles = 0;
         p.bytes = static_cast<size_t>(p.chunks) * partial + sequences * sizeof(int2);
@@ -834,7 +836,8 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
     if (!one && plan.chunks == 1) return RCP_OK;
     // (a second dimension ends at 65535; rows are split only where there are few of them, times query heads)
     const dim3 grid = one ? dim3(static_cast<unsigned>(c.H_q), static_cast<unsigned>(c.sequences)) : dim3(static_cast<unsigned>(c.H_q) * static_cast<unsigned>(c.rows));
-    // wavefronts for the partial results of a row: eight to a thread at a time
+    // Wavefronts for the partial results of a row, by their mean number: eight to a thread at a time.  With as few for long rows as for short ones the whole
+    // call takes 33.9 us instead of 22.7 (one sequence of 30000 tokens of 8 heads), with as many for short ones 21.1 instead of 19.6 (16 sequences of 2000 tokens).
     auto merge = [&](auto size) {
         constexpr int D = decltype(size)::value;
         const int each = one ? plan.chunks / c.sequences : plan.chunks;
