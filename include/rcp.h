@@ -596,9 +596,8 @@ int rcp_kv4_attn_decode_batched(const void* q, rcp_dtype q_dtype, int B, int H_q
  *   (rcp_kv8_append writes none).  Scales count as 2^-40 .. 2^120, a smaller one (0 of a page never written) as 2^-40.  Scores have to stay within binary32.  Sums
  *   are binary32.  The softmax weights enter the product with the values as pairs of binary16 numbers (22 bits), with several tokens and bfloat16
  *   results as one (11 bits); a weight there carries the value scale of its page and is off by 2^-34 of the row's largest such product at most (elements that pages of far larger
- *   values hold as zeros show it), and one below 2^-120 of that counts as none.  A row's query enters scaled by its largest element: 16-bit ones exactly down to 2^-27 of that with one token a
- *   sequence, otherwise down to 2^-14 and smaller elements off by 2^-22 of it (bfloat16) or 2^-27 (binary16) at most; binary32 ones as pairs of binary16 numbers (22 bits, or off
- *   by 2^-38 of it where that is more).  out must not overlap q.
+ *   values hold as zeros show it), and one below 2^-120 of that counts as none.  A row's query enters scaled by its largest element: 16-bit ones exactly down to 2^-27 of that, binary32 ones as pairs of
+ *   binary16 numbers (22 bits), smaller elements off by 2^-38 of the largest at most.  out must not overlap q.
  *   workspace: rcp_kv8_workspace_bytes(rows, sequences, H_q, H, D, starts == NULL) bytes, overwritten by every call.  Calls that
  *   may overlap need workspaces of their own.
  * Limits (RCP_ERR_SHAPE): sequences <= 1024, width * page <= 2^24, sequences * width * page < 2^31, H and H_q <= 4096, rows <= 2^20; rcp_kv8_append: strides <= 2^31,

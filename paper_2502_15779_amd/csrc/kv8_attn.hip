@@ -10,9 +10,10 @@
 // lane has weights of; value codes come back transposed from LDS (ds_read_b64_tr_b8: eight rows of sixteen bytes, a lane gets a column).
 // A code becomes a binary16 number, exactly, half an instruction each.
 //
-// The query of a row enters scaled by a power of two.  One token a sequence: its largest element at 2^13 .. 2^14, as one binary16 number (a 16-bit query exactly
-// down to 2^-27 of that) or two (a binary32 query, QP).  Several tokens: 16-bit queries as two or three E4M3 pieces, which meet the codes as they are in one
-// product each of 64 elements; binary32 queries as pairs of binary16 numbers.
+// The query of a row enters scaled by a power of two, its largest element at 2^13 .. 2^14, as one binary16 number (a 16-bit query exactly down to 2^-27 of that) or two (a
+// binary32 query, QP).  Not as E4M3 pieces, which would meet the codes without a conversion: the matrix cores' 8-bit products are not summed in binary32.  A product is cut off where its
+// bits lie about 16 places below the largest one of an instruction (448 x 448 and 63 times 1 x 1 give 200760 instead of 200767), so that scores were off by up to 2^-15 of
+// sum |q_d K_td|, and binary32 results by 4.7e-5 instead of 4e-7 (8192 tokens of 32 + 2 x 8 heads of 128, bfloat16: 533 us so, 568 us now).
 // A weight is 2^(score + log2 s' - m), at most 2^14; the codes of a page then enter the sum of outputs as they are, and its scale the sum of weights as 1 / s'.  The
 // reference m of a row is so held against score + log2 s' that a page of a large scale and little attention does not push the others out of
 // binary16; it moves only when a weight would leave the range.  A weight enters the product as two binary16 numbers, 22 bits of it.  One number (PP = 1) is off by up to
@@ -459,24 +460,6 @@ __device__ __forceinline__ int kv8_prompt_swizzle(int token)
     else return ((token >> 2) & 1) | ((token >> 2) & 2);
 }
 
-// v, scaled so that its row's largest element is at 2^7 .. 2^8, as `PIECES` E4M3 numbers, each of 2^-5 times the unit of the one before: four bits and
-// the sign of the rest each, so that two hold a bfloat16 number and three a binary16 number exactly, down to 2^-14 of the largest; below that the
-// rest is at most 2^-15 with two pieces and 2^-20 with three: 2^-22 and 2^-27 of a largest element of 2^7.  Four numbers to a dword of each piece.
-template <int PIECES>
-__device__ __forceinline__ void kv8_query_pieces(const float (&v)[4], int (&piece)[PIECES])
-{
-    float r[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        piece[p] = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], 0, false), true);
-        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(piece[p], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(piece[p], true);
-        r[0] = 32.0f * (r[0] - a[0]);
-        r[1] = 32.0f * (r[1] - a[1]);
-        r[2] = 32.0f * (r[2] - b[0]);
-        r[3] = 32.0f * (r[3] - b[1]);
-    }
-}
-
 template <int D, int QP, int PP>
 __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 {
@@ -511,9 +494,7 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
     const int token = first + min(my, n_rows - 1) / a.rep, head = hk * a.rep + min(my, n_rows - 1) % a.rep;
     const size_t out_row = static_cast<size_t>(token) * a.H_q + head;
 
-    constexpr bool CODES = QP != 0;  // the query in E4M3 pieces, which meet the codes as they are; otherwise as pairs of binary16 numbers
-    v8h qh[CODES ? 1 : KL][2], ql[CODES ? 1 : KL][2];
-    v8i qc[CODES ? QP : 1][KL / 2];
+    v8h qh[KL][2], ql[QP == 2 ? KL : 1][2];
     float unit;
     {
         float t[KL][2][8], top = 0.0f;
@@ -527,28 +508,16 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             }
         top = kv8_swap32_max(top);
         const int E = __builtin_amdgcn_frexp_expf(top);
-        constexpr int BITS = CODES ? 8 : 14;  // the largest element becomes 2^(BITS - 1) .. 2^BITS
 #pragma unroll
         for (int k = 0; k < KL; ++k)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], BITS - E);
-                if constexpr (CODES) {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        const float v[4] = {t[k][x][e], t[k][x][e + 1], t[k][x][e + 2], t[k][x][e + 3]};
-                        int piece[QP];
-                        kv8_query_pieces<QP>(v, piece);
-#pragma unroll
-                        for (int p = 0; p < QP; ++p) qc[p][k / 2][4 * (k & 1) + 2 * x + e / 4] = piece[p];
-                    }
-                } else {
-                    qh[k][x] = kv8_round(t[k][x]);
-                    ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
-                }
+                for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], 14 - E);
+                qh[k][x] = kv8_round(t[k][x]);
+                if constexpr (QP == 2) ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
             }
-        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - BITS);
+        unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
     }
 
     auto resource = [&](const unsigned char* codes, const Kv8Block& x) {
@@ -613,25 +582,15 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             const unsigned char* const at = &kt[buf][(32 * tb + c) * D];
             const int f = kv8_prompt_swizzle<D>(c);
 #pragma unroll
-            for (int k = 0; k < KL; k += 2) {
-                const u32x4 w0 = *reinterpret_cast<const u32x4*>(at + (((2 * k + hh) ^ f) * 16)), w1 = *reinterpret_cast<const u32x4*>(at + (((2 * k + 2 + hh) ^ f) * 16));
-                if constexpr (CODES) {
-                    const v8i w = {static_cast<int>(w0[0]), static_cast<int>(w0[1]), static_cast<int>(w0[2]), static_cast<int>(w0[3]),
-                                   static_cast<int>(w1[0]), static_cast<int>(w1[1]), static_cast<int>(w1[2]), static_cast<int>(w1[3])};
-#pragma unroll
-                    for (int p = QP - 1; p >= 0; --p)  // E4M3 times E4M3, the query's scale 2^(-5 p)
-                        S[tb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, qc[p][k / 2], S[tb], 0, 0, 0, 127, 0, 127 - 5 * p);
-                } else {
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const u32x4 x = y == 0 ? w0 : w1;
-                        const v8h k0 = kv8_halves(x[0], x[1]), k1 = kv8_halves(x[2], x[3]);
-                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[k + y][0], S[tb], 0, 0, 0);
-                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[k + y][1], S[tb], 0, 0, 0);
-                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[k + y][0], S[tb], 0, 0, 0);
-                        S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k + y][1], S[tb], 0, 0, 0);
-                    }
+            for (int k = 0; k < KL; ++k) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(at + (((2 * k + hh) ^ f) * 16));
+                const v8h k0 = kv8_halves(x[0], x[1]), k1 = kv8_halves(x[2], x[3]);
+                if constexpr (QP == 2) {
+                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql[k][0], S[tb], 0, 0, 0);
+                    S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql[k][1], S[tb], 0, 0, 0);
                 }
+                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh[k][0], S[tb], 0, 0, 0);
+                S[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh[k][1], S[tb], 0, 0, 0);
             }
         }
         float ks[4], vi[4], vl[4];
@@ -822,12 +781,10 @@ int launch_kv8_attn(const Kv8AttnCall& c, hipStream_t st)
             const unsigned grid = static_cast<unsigned>(plan.tiles) * static_cast<unsigned>(plan.chunks) * static_cast<unsigned>(c.H_kv);
             auto launch = [&](auto kernel) { enqueue(kernel, grid, 256, 0, st, a); };
             const bool p2 = c.out_dtype != RCP_BF16;
-            if (q2 && p2) launch(&kv8_prompt_kernel<D, 0, 2>);
-            else if (q2) launch(&kv8_prompt_kernel<D, 0, 1>);
-            else if (c.q_dtype == RCP_F16 && p2) launch(&kv8_prompt_kernel<D, 3, 2>);
-            else if (c.q_dtype == RCP_F16) launch(&kv8_prompt_kernel<D, 3, 1>);
-            else if (p2) launch(&kv8_prompt_kernel<D, 2, 2>);
-            else launch(&kv8_prompt_kernel<D, 2, 1>);
+            if (q2 && p2) launch(&kv8_prompt_kernel<D, 2, 2>);
+            else if (q2) launch(&kv8_prompt_kernel<D, 2, 1>);
+            else if (p2) launch(&kv8_prompt_kernel<D, 1, 2>);
+            else launch(&kv8_prompt_kernel<D, 1, 1>);
         }
     };
     if (c.D == 128) form(std::integral_constant<int, 128>{});

@@ -28,10 +28,10 @@ def _score(q, code, scale, one):
     return torch.log(out * (seen - 1) / (1 - out))
 
 
-@pytest.mark.parametrize("one,dtype,bound", [(False, "bf16", 2.0 ** -22), (False, "f16", 2.0 ** -27), (True, "bf16", 2.0 ** -38), (True, "f16", 2.0 ** -38),
-                                             (False, "f32", 2.0 ** -38), (True, "f32", 2.0 ** -38)])
-def test_small_elements_beside_a_large_one(one, dtype, bound):
-    """Elements of 2^-14 to 2^-29 of the largest, with all the bits of their type: off by `bound` of the largest at most (pairs of binary16 numbers: or by 2^-22 of themselves)."""
+@pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_small_elements_beside_a_large_one(one, dtype):
+    """Elements of 2^-14 to 2^-29 of the largest, with all the bits of their type: off by 2^-38 of the largest at most (pairs of binary16 numbers: or by 2^-22 of themselves)."""
     dtype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[dtype]
     g = torch.Generator().manual_seed(7)
     largest, rows, H_q, D = 2.0 ** 15, 8, 16, 64
@@ -49,6 +49,4 @@ def test_small_elements_beside_a_large_one(one, dtype, bound):
         # the score's own binary32 steps, and the result's: 1 / (1 + e^-s) is at least 0.1 away from 0 and 1, rounded a few times
         off = (got - exact).abs() - (2.0 ** -19 + 2.0 ** -22 * exact)
         worst = max(worst, float((off / (16 * scale * largest)).max()))
-    assert worst <= bound, f"2^{float(torch.tensor(worst).log2()):.2f} of the largest element"
-    if not one and dtype == torch.bfloat16:
-        assert worst > 2.0 ** -22.1
+    assert worst <= 2.0 ** -38, f"2^{float(torch.tensor(worst).log2()):.2f} of the largest element"
