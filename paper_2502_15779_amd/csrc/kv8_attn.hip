@@ -18,9 +18,9 @@
 // reference m of a row is so held against score + log2 s' that a page of a large scale and little attention does not push the others out of
 // binary16; it moves only when a weight would leave the range.  A weight enters the product as two binary16 numbers, 22 bits of it.  One number (PP = 1) is off by up to
 // 2^-11 of the weight, and only several tokens with bfloat16 results, whose own half step is 2^-8, take it: there the second product of each block costs a third (8192 tokens of 32 + 2 x 8 heads
-// of 128: 541 us with one number, 738 with two) and changes the error against 64 bits by less than a hundredth.  For binary16 results it would be as large as the result's own rounding,
-// and more where values cancel (three chunks behind 5000 to 17003 tokens, heads of 64: 62 us and an error of 2.4e-4 with one, 80 us and 2.1e-4 with two); single
-// tokens hardly pay for it (16 sequences of up to 6000 tokens 27.4 us with one, 28.3 with two).  The range of binary16 ends below, too: with a row's largest weight at
+// of 128: 571 us with one number, 755 with two) and changes the error against 64 bits by less than a hundredth.  For binary16 results it would be as large as the result's own rounding,
+// and more where values cancel (three chunks behind 5000 to 17003 tokens, heads of 64: 62 us and an error of 2.3e-4 with one, 74 us and 2.1e-4 with two); single
+// tokens hardly pay for it (16 sequences of up to 6000 tokens 27.4 us with one, 28.1 with two).  The range of binary16 ends below, too: with a row's largest weight at
 // 2^9 .. 2^14, one number has its 11 bits down to 2^-23 of that (two their 22 bits down to 2^-12), and either form is off by 2^-34 of it at most.  Since a weight carries its page's
 // scale, this can only show in elements that are zero in all tokens of a large weight times scale, beside tokens 2^12, or 2^23, times smaller.  Sums are binary32.
 #include <math.h>
@@ -66,12 +66,17 @@ __device__ __forceinline__ v8h kv8_round(const float (&v)[8])
     for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e]);
     return h;
 }
-__device__ __forceinline__ v8h kv8_rest(const float (&v)[8], const v8h& h)
+__device__ __forceinline__ void kv8_split(const float (&v)[8], v8h& h, v8h& rest)
 {
-    v8h r;
+    u32x4 w = __builtin_bit_cast(u32x4, kv8_round(v));
+    // The rest in one instruction, a multiply-add that takes a half of a register for a factor.  (Hidden from the compiler: that the halves are v's, which it would convert a
+    // second time, alone, and that the other factor is -1, since it would turn a subtraction into two instructions.)
+    float minus = -1.0f;
+    asm("" : "+v"(w));
+    asm("" : "+s"(minus));
+    h = __builtin_bit_cast(v8h, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = static_cast<_Float16>(v[e] - static_cast<float>(h[e]));
-    return r;
+    for (int e = 0; e < 8; ++e) rest[e] = static_cast<_Float16>(fmaf(static_cast<float>(h[e]), minus, v[e]));
 }
 
 // eight query elements from index i on
@@ -261,8 +266,8 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
         for (int d = 0; d < 2 * KX; ++d) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) t[d][e] = ldexpf(t[d][e], 14 - E);
-            qh[d] = kv8_round(t[d]);
-            if constexpr (QP == 2) ql[d] = kv8_rest(t[d], qh[d]);
+            if constexpr (QP == 2) kv8_split(t[d], qh[d], ql[d]);
+            else qh[d] = kv8_round(t[d]);
         }
         unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
     }
@@ -331,8 +336,7 @@ __global__ __launch_bounds__(64) void kv8_decode_kernel(Kv8AttnArgs a)
             }
             l = fmaf((w[0] + w[1]) + (w[2] + w[3]), vs[2 * s], l);
             l = fmaf((w[4] + w[5]) + (w[6] + w[7]), vs[2 * s + 1], l);
-            ph[s] = kv8_round(w);
-            pl[s] = kv8_rest(w, ph[s]);
+            kv8_split(w, ph[s], pl[s]);
         }
         // the values of this tile are in LDS once no more loads than the keys requested above are outstanding
         __builtin_amdgcn_sched_barrier(0);
@@ -514,8 +518,8 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) t[k][x][e] = ldexpf(t[k][x][e], 14 - E);
-                qh[k][x] = kv8_round(t[k][x]);
-                if constexpr (QP == 2) ql[k][x] = kv8_rest(t[k][x], qh[k][x]);
+                if constexpr (QP == 2) kv8_split(t[k][x], qh[k][x], ql[k][x]);
+                else qh[k][x] = kv8_round(t[k][x]);
             }
         unit = ldexpf(a.softmax_scale * KV8_LOG2E, E - 14);
     }
@@ -641,9 +645,9 @@ __global__ __launch_bounds__(256) void kv8_prompt_kernel(Kv8AttnArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(S[n >> 1][8 * (n & 1) + e], by[n], less));
             l = fmaf(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])), vi[n], l);
-            const v8h ph = kv8_round(w);
-            v8h pl;
-            if constexpr (PP == 2) pl = kv8_rest(w, ph);
+            v8h ph, pl;
+            if constexpr (PP == 2) kv8_split(w, ph, pl);
+            else ph = kv8_round(w);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
