@@ -218,7 +218,8 @@ __device__ __forceinline__ void kv8_queries(const Kv8AppendArgs& a, int block)
 }
 
 // One new token a sequence: a vector is all that its page and head gets, so that its lanes need no other wavefront.
-// Bound by the launch and one chain of loads, length -> page -> scale and codes: 2.8 us (one sequence of 32 + 2 x 32 heads of 128), 3.3 us (16 of 32 + 2 x 8).
+// Bound by the launch and one chain of loads, length -> page -> scale and codes: 2.7 us (one sequence of 32 + 2 x 32 heads of 128), 3.3 us (16 of 32 + 2 x 8).
+// So where no scale grows.  A page whose scale does has its older codes read and written, eight at a time: 12.9 and 13.4 us if that is every page, with 63 older tokens in each.
 template <int DT, int D>
 __global__ __launch_bounds__(256) void kv8_append_one_kernel(Kv8AppendArgs a)
 {
@@ -259,7 +260,8 @@ __global__ __launch_bounds__(256) void kv8_append_one_kernel(Kv8AppendArgs a)
     if (l == 0 && scale != old) *scale_at = scale;
 }
 
-// Bound by memory: 7273 tokens of 32 + 2 x 8 heads of 128 in bfloat16 read and write 167 MB in 40.7 us, 4.1 TB/s, where a copy reaches 4.6.
+// Bound by memory: 7273 tokens of 32 + 2 x 8 heads of 128 in bfloat16 read and write 167 MB in 40.7 us, 4.1 TB/s, where a copy reaches 4.6 (the
+// same within a hundredth where the scale of every page with older tokens grows: they are seven of 230).
 // Several new tokens of a sequence: a workgroup owns one page of one head, keeps its new tokens in registers (PASSES vectors a lane) until
 // their largest magnitude is known, and writes them together.
 template <int DT, int D, int PASSES>

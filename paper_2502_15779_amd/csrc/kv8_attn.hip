@@ -154,8 +154,8 @@ __device__ __forceinline__ void kv8_to_lds_once(__amdgpu_buffer_rsrc_t from, uns
 // ---------------------------------------------------------------------------------------
 // One new token a sequence.  Workgroup = one wavefront = (chunk of cached tokens of a sequence, cache head [, sixteen of its query heads]); the chunks are
 // cut on the device from the lengths, so that a captured call stays balanced when they change.  16x16x32 products: a lane holds the row (query
-// head) lane % 16.  Bound by the reads of codes: 103 MB (16 sequences of up to 6000 tokens, 8 heads of 128) in 23.6 us, 4.4 TB/s, and 4.6 us for the merge; 33 MB (one
-// sequence, 32 heads) in 10.8 us, of which half are the start and the chain length -> page -> codes.  Why a wavefront a workgroup: with four and a common
+// head) lane % 16.  Bound by the reads of codes: 103 MB (16 sequences of up to 6000 tokens, 8 heads of 128) in 23.8 us, 4.3 TB/s, and 4.6 us for the merge; 33 MB (one
+// sequence, 32 heads) in 10.9 us, of which half are the start and the chain length -> page -> codes.  Why a wavefront a workgroup: with four and a common
 // chunk, a barrier in each tile made all wait for the slowest load (31.5 us instead of 28, merge included).
 // ---------------------------------------------------------------------------------------
 
@@ -451,8 +451,8 @@ __global__ __launch_bounds__(GROUPS * D) void kv8_decode_merge_kernel(Kv8AttnArg
 // the cached tokens]); row = (new token, query head of the group).  32x32x16 products: a lane holds the row lane % 32 of its
 // wavefront's 32 and, of each 32 tokens, those with (token / 4) % 2 = lane / 32.  The four wavefronts share the tiles of 64 tokens in LDS, four of them, of which
 // three are under way (the compiler waits for them before the transposing reads; loads behind those reads measure the same).  Bound by the vector unit (a conversion to binary16, a multiply-add, an exponential, a rounding, the maximum and the sum of each
-// score and value) together with the matrix cores: busy 68 and 47 % of the cycles.  8192 tokens of 32 + 2 x 8 heads of 128: 550 GFLOP in 538 .. 592 us, 0.93 ..
-// 1.02 PFLOP/s; four prompts of 301 to 2000 tokens 56 GFLOP in 86 .. 98 us.
+// score and value) together with the matrix cores: busy 76 and 46 % of the cycles.  8192 tokens of 32 + 2 x 8 heads of 128, bfloat16: 550 GFLOP in 568 .. 639 us, 0.86 ..
+// 0.97 PFLOP/s; binary32 queries and results 911 us, binary16 ones 759.  Four prompts of 301 to 2000 tokens, bfloat16: 56 GFLOP in 89 .. 100 us.
 // ---------------------------------------------------------------------------------------
 constexpr int KV8_ROWS = 128;
 constexpr int KV8_STAGES = 4;  // tiles in LDS: one in use, the others under way
